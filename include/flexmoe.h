@@ -53,7 +53,8 @@ enum flexmoe_status {
 };
 
 enum flexmoe_dtype { FLEXMOE_F32 = 0, FLEXMOE_BF16 = 1 };
-enum flexmoe_act { FLEXMOE_RELU = 0, FLEXMOE_GELU_ERF = 1, FLEXMOE_GELU_TANH = 2 };
+/* FLEXMOE_SILU (z / (1 + e^-z)): gated and 8-bit expert calls only. */
+enum flexmoe_act { FLEXMOE_RELU = 0, FLEXMOE_GELU_ERF = 1, FLEXMOE_GELU_TANH = 2, FLEXMOE_SILU = 3 };
 
 /* Human-readable name of a status code (static storage). */
 const char* flexmoe_status_str(int status);
@@ -153,6 +154,37 @@ int flexmoe_expert_ffn_bwd_top1(const void* dyp, const void* xp, const void* hpr
                                 const int32_t* vexpert_off, const int32_t* vexpert_owner, const int32_t* src,
                                 int N, int d, int f, int E, int V, int act, int dtype,
                                 void* dx, void* dw1, void* dw2, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated expert FFN forward (experts with two first projections, e.g. SwiGLU: act = FLEXMOE_SILU), per bucket v owned by expert e:
+ *   [G | U] = xp[rows_v,:] . W1_e + b1_e ;  H = act(G) * U ;  yp[rows_v,:] = H . W2_e + b2_e
+ *   xp [A,d], w1 [E,d,2f] (columns 0..f-1 give G, f..2f-1 give U), b1 [E,2f] or NULL, w2 [E,f,d], b2 [E,d] or NULL, all dtype;
+ *   vexpert_off [V+1], vexpert_owner [V] as written by flexmoe_route.
+ *   -> hpre [A,2f] dtype ([G | U], for the backward pass) or NULL (inference: not stored, yp is the same bit for bit),
+ *      h [A,f] dtype or NULL (H, kept for the backward pass; NULL: in the workspace), yp [A,d] dtype.
+ * act: any of flexmoe_act.  H is computed in fp32 from the products' fp32 sums and rounded once, so with bf16 it is not bit for bit what
+ * the rounded [G | U] would give.
+ * ws: at least flexmoe_workspace_bytes(N, d, 2 * f, E, k, V, dtype) bytes, as for flexmoe_expert_ffn_gated_bwd.
+ * d and f are multiples of 8 below 2^20.  Equal calls give equal bits; as in flexmoe_expert_ffn_fwd, a row's last bits may depend on the
+ * bucket sizes.
+ */
+int flexmoe_expert_ffn_gated_fwd(const void* xp, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1,
+                                 const void* b1, const void* w2, const void* b2, int A, int d, int f, int E, int V, int act,
+                                 int dtype, void* hpre, void* h, void* yp, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated expert FFN backward for upstream gradient dyp [A,d]:
+ *   dH = dyp . W2_e^T ; dG = dH * U * act'(G) ; dU = dH * act(G) ; dHpre = [dG | dU] ; dxp = dHpre . W1_e^T
+ *   dw2[e] [f,d] = sum over e's buckets of H_v^T . dyp_v ;  dw1[e] [d,2f] = sum over e's buckets of xp_v^T . dHpre_v
+ *   (ascending vExpert id, fp32 accumulation; overwritten, zeros for experts without tokens)
+ *   hpre [A,2f] as the forward call left it.  h [A,f]: H as the forward call left it, or NULL: computed again from hpre (with bf16 from
+ *   rounded values, so dw2 then differs by that rounding).
+ * ws as in the forward call; afterwards dHpre [A,2f] is at its start, and flexmoe_expert_bias_grads called next with 2f in the place of f
+ * gives db1 [E,2f] and db2.
+ */
+int flexmoe_expert_ffn_gated_bwd(const void* dyp, const void* xp, const void* hpre, const void* h, const void* w1, const void* w2,
+                                 const int32_t* vexpert_off, const int32_t* vexpert_owner, int A, int d, int f, int E, int V,
+                                 int act, int dtype, void* dxp, void* dw1, void* dw2, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Reverse routing and gate-weighted sum, Eq. 4:

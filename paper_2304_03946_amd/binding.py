@@ -17,13 +17,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libflexmoe.so")
 
 F32, BF16 = 0, 1
-RELU, GELU_ERF, GELU_TANH = 0, 1, 2
+RELU, GELU_ERF, GELU_TANH, SILU = 0, 1, 2, 3
 OK, INVALID_ARG, BAD_PLACEMENT, WORKSPACE_TOO_SMALL, UNSUPPORTED, DEVICE_ERROR, SCRATCH_LIMIT = range(7)
 
 EXPORTS = ["flexmoe_status_str", "flexmoe_workspace_bytes", "flexmoe_gate_topk", "flexmoe_route",
            "flexmoe_permute", "flexmoe_expert_ffn_fwd", "flexmoe_expert_ffn_bwd", "flexmoe_combine",
            "flexmoe_gate_bwd", "flexmoe_expert_bias_grads", "flexmoe_expert_ffn_fwd_gather",
            "flexmoe_expert_ffn_fwd_top1", "flexmoe_expert_ffn_bwd_top1", "flexmoe_route_static",
+           "flexmoe_expert_ffn_gated_fwd", "flexmoe_expert_ffn_gated_bwd",
            # host-side scheduler (include/flexmoe_scheduler.h; Python face in scheduler.py)
            "flexmoe_balance_ratio", "flexmoe_step_cost", "flexmoe_make_scheduling_plan", "flexmoe_schedule",
            "flexmoe_placement_table"]
@@ -73,6 +74,10 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.flexmoe_expert_ffn_fwd_top1.argtypes = [c_vp] * 8 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_expert_ffn_bwd_top1.restype = c_int
     lib.flexmoe_expert_ffn_bwd_top1.argtypes = [c_vp] * 9 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.flexmoe_expert_ffn_gated_fwd.restype = c_int
+    lib.flexmoe_expert_ffn_gated_fwd.argtypes = [c_vp] * 7 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.flexmoe_expert_ffn_gated_bwd.restype = c_int
+    lib.flexmoe_expert_ffn_gated_bwd.argtypes = [c_vp] * 8 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_gate_bwd.restype = c_int
     lib.flexmoe_gate_bwd.argtypes = [c_vp] * 10 + [c_int] * 6 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_expert_bias_grads.restype = c_int
@@ -223,6 +228,27 @@ def flexmoe_expert_ffn_bwd(dyp, xp, hpre, w1, w2, vexpert_off, vexpert_owner, ac
                                                _ptr(vexpert_owner), A, d, f, E, V, act, dtype_code(xp), _ptr(dxp),
                                                _ptr(dw1), _ptr(dw2), _ptr(ws), ws.nbytes, _stream())
     _check(st, "flexmoe_expert_ffn_bwd")
+
+
+def flexmoe_expert_ffn_gated_fwd(xp, vexpert_off, vexpert_owner, w1, b1, w2, b2, act, hpre, yp, ws, h=None):
+    A, d = xp.shape
+    E, f, _ = w2.shape
+    V = vexpert_owner.shape[0]
+    st = load_library().flexmoe_expert_ffn_gated_fwd(_ptr(xp), _ptr(vexpert_off), _ptr(vexpert_owner), _ptr(w1), _ptr(b1),
+                                                     _ptr(w2), _ptr(b2), A, d, f, E, V, act, dtype_code(xp), _ptr(hpre),
+                                                     _ptr(h), _ptr(yp), _ptr(ws), ws.nbytes, _stream())
+    _check(st, "flexmoe_expert_ffn_gated_fwd")
+
+
+def flexmoe_expert_ffn_gated_bwd(dyp, xp, hpre, w1, w2, vexpert_off, vexpert_owner, act, dxp, dw1, dw2, ws, h=None):
+    A, d = xp.shape
+    E, f, _ = w2.shape
+    V = vexpert_owner.shape[0]
+    st = load_library().flexmoe_expert_ffn_gated_bwd(_ptr(dyp), _ptr(xp), _ptr(hpre), _ptr(h), _ptr(w1), _ptr(w2),
+                                                     _ptr(vexpert_off), _ptr(vexpert_owner), A, d, f, E, V, act,
+                                                     dtype_code(xp), _ptr(dxp), _ptr(dw1), _ptr(dw2), _ptr(ws), ws.nbytes,
+                                                     _stream())
+    _check(st, "flexmoe_expert_ffn_gated_bwd")
 
 
 def flexmoe_gate_bwd(wg, topk_idx, topk_w, dy, yp, xp, dest, src, vexpert_off, vexpert_owner, dl, dx, dwg, ws):

@@ -8,6 +8,7 @@ namespace {
 
 bool dtype_ok(int dtype) { return dtype == FLEXMOE_F32 || dtype == FLEXMOE_BF16; }
 bool act_ok(int act) { return act == FLEXMOE_RELU || act == FLEXMOE_GELU_ERF || act == FLEXMOE_GELU_TANH; }
+bool gate_act_ok(int act) { return act_ok(act) || act == FLEXMOE_SILU; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int dims_status(int N, int d, int f, int E, int k, int V) {
@@ -129,6 +130,8 @@ int flexmoe_combine(const void* yp, const int32_t* dest, const float* topk_w, in
   return dev_status(launch_combine(yp, dest, topk_w, N, k, d, dtype, y, (hipStream_t)stream));
 }
 
+constexpr int kMaxWidth = 1 << 20;      // of gated and 8-bit layers (flexmoe.h)
+
 static int ffn_common(int A, int d, int f, int E, int V, int act, int dtype, const void* voff, const void* owner,
                       const void* ws, size_t ws_bytes) {
   if (!dtype_ok(dtype) || !act_ok(act)) return FLEXMOE_UNSUPPORTED;
@@ -220,6 +223,45 @@ int flexmoe_expert_ffn_bwd_top1(const void* dyp, const void* xp, const void* hpr
     return FLEXMOE_INVALID_ARG;
   const FfnArgs a{N, d, f, E, V, act, vexpert_off, vexpert_owner};
   return dev_status(launch_ffn_bwd_bf16(a, dyp, xp, hpre, h, w1, w2, dx, dw1, dw2, ws, (hipStream_t)stream, src));
+}
+
+// (the workspace is that of a layer with 2 f columns; f first: 2 f must not overflow)
+static int gated_common(int A, int d, int f, int E, int V, int act, int dtype, const void* voff, const void* owner, const void* ws,
+                        size_t ws_bytes) {
+  if (!gate_act_ok(act)) return FLEXMOE_UNSUPPORTED;
+  if (f >= kMaxWidth || d >= kMaxWidth) return FLEXMOE_INVALID_ARG;
+  if (f < 8 || f % 8) return FLEXMOE_INVALID_ARG;
+  return ffn_common(A, d, 2 * f, E, V, FLEXMOE_RELU, dtype, voff, owner, ws, ws_bytes);
+}
+
+int flexmoe_expert_ffn_gated_fwd(const void* xp, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1,
+                                 const void* b1, const void* w2, const void* b2, int A, int d, int f, int E, int V, int act,
+                                 int dtype, void* hpre, void* h, void* yp, void* ws, size_t ws_bytes, void* stream) {
+  const int st = gated_common(A, d, f, E, V, act, dtype, vexpert_off, vexpert_owner, ws, ws_bytes);
+  if (st != FLEXMOE_OK) return st;
+  if (!w1 || !w2 || !aligned16(w1) || !aligned16(w2) || !aligned16(b1) || !aligned16(b2)) return FLEXMOE_INVALID_ARG;
+  if (A > 0 && (!xp || !yp || !aligned16(xp) || !aligned16(hpre) || !aligned16(h) || !aligned16(yp)))      // hpre, h may be NULL
+    return FLEXMOE_INVALID_ARG;
+  const FfnArgs a{A, d, f, E, V, act, vexpert_off, vexpert_owner};
+  const hipStream_t s = (hipStream_t)stream;
+  return dev_status(dtype == FLEXMOE_BF16 ? launch_ffn_gated_fwd_bf16(a, xp, w1, b1, w2, b2, hpre, h, yp, ws, s)
+                                          : launch_ffn_gated_fwd_f32(a, xp, w1, b1, w2, b2, hpre, h, yp, ws, s));
+}
+
+int flexmoe_expert_ffn_gated_bwd(const void* dyp, const void* xp, const void* hpre, const void* h, const void* w1, const void* w2,
+                                 const int32_t* vexpert_off, const int32_t* vexpert_owner, int A, int d, int f, int E, int V,
+                                 int act, int dtype, void* dxp, void* dw1, void* dw2, void* ws, size_t ws_bytes, void* stream) {
+  const int st = gated_common(A, d, f, E, V, act, dtype, vexpert_off, vexpert_owner, ws, ws_bytes);
+  if (st != FLEXMOE_OK) return st;
+  if (!w1 || !w2 || !dw1 || !dw2 || !aligned16(w1) || !aligned16(w2) || !aligned16(dw1) || !aligned16(dw2))
+    return FLEXMOE_INVALID_ARG;
+  if (A > 0 && (!dyp || !xp || !hpre || !dxp || !aligned16(dyp) || !aligned16(xp) || !aligned16(hpre) || !aligned16(h) ||
+                !aligned16(dxp)))      // h may be NULL
+    return FLEXMOE_INVALID_ARG;
+  const FfnArgs a{A, d, f, E, V, act, vexpert_off, vexpert_owner};
+  const hipStream_t s = (hipStream_t)stream;
+  return dev_status(dtype == FLEXMOE_BF16 ? launch_ffn_gated_bwd_bf16(a, dyp, xp, hpre, h, w1, w2, dxp, dw1, dw2, ws, s)
+                                          : launch_ffn_gated_bwd_f32(a, dyp, xp, hpre, h, w1, w2, dxp, dw1, dw2, ws, s));
 }
 
 int flexmoe_gate_bwd(const void* wg, const int32_t* topk_idx, const float* topk_w, const void* dy, const void* yp,

@@ -12,6 +12,8 @@ typedef unsigned short bf16_t;   // bf16 bit pattern
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWave = 64;
 
@@ -191,5 +193,14 @@ hipError_t launch_ffn_fwd_f32(const FfnArgs& a, const void* xp, const void* w1, 
 hipError_t launch_ffn_bwd_f32(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept,
                               const void* w1, const void* w2, void* dxp, void* dw1, void* dw2,
                               void* ws, hipStream_t s);
+// gated experts: a.f columns of H, w1 [E, d, 2 f], hpre [A, 2 f]; ws as for a layer of 2 f
+hipError_t launch_ffn_gated_fwd_bf16(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
+                                     void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s);
+hipError_t launch_ffn_gated_bwd_bf16(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept, const void* w1,
+                                     const void* w2, void* dxp, void* dw1, void* dw2, void* ws, hipStream_t s);
+hipError_t launch_ffn_gated_fwd_f32(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
+                                    void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s);
+hipError_t launch_ffn_gated_bwd_f32(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept, const void* w1,
+                                    const void* w2, void* dxp, void* dw1, void* dw2, void* ws, hipStream_t s);
 
 }  // namespace flexmoe

@@ -55,6 +55,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "ffn_bf16_host.h"
 #include "ffn_bf16_tile.h"
 #include "ffn_bf16_dma.h"
 #include "ffn_bf16_persist.h"
@@ -273,10 +274,17 @@ static int plan_blocks(const FfnArgs& a) {
 }
 // What the rows kernels of one forward call look up: the row-tile table of the persistent kernels, or the small kernels'
 // row list.
-static void launch_rows_plan(const FfnArgs& a, void* ws, hipStream_t s) {
+void launch_rows_plan(const FfnArgs& a, void* ws, hipStream_t s) {
   const SmallPlan small = small_plan_ws(a, ws);
   if (small.bm) hipLaunchKernelGGL(small_plan_kernel, dim3(plan_blocks(a)), dim3(kGemmThreads), 0, s, a.voff, a.owner, a.E, a.V, small);
   else hipLaunchKernelGGL(rows_plan_kernel, dim3(plan_blocks(a)), dim3(kGemmThreads), 0, s, a.voff, a.owner, a.V, rows_tab_ws(a, ws));
+}
+
+RowsKernels rows_kernels(const FfnArgs& a, void* ws) {
+  RowsKernels r;
+  r.small = small_plan_ws(a, ws, &r.small_partial);
+  r.row_tab = rows_tab_ws(a, ws);
+  return r;
 }
 
 template <bool WT, int EPI, bool EVAL>
@@ -399,20 +407,19 @@ static WgradDmaArgs wgrad_dma_args(const FfnArgs& a, const void* L, const void* 
 }
 
 // How the work lists of dW2 and dW1 are balanced (only the persistent kernels skip the holes that balancing leaves in a list).
-static void wgrad_balance(const FfnArgs& a, WgradBalance* geo) {
-  const int f_tiles = (a.f + BM - 1) / BM, d_tiles = (a.d + BM - 1) / BM;
-  const bool whole = a.f % BM == 0 && a.d % BN == 0 && !wgrad_small(a.A, a.d, a.f, a.E);
-  geo[0] = whole ? wgrad_balance_geometry(f_tiles, d_tiles) : WgradBalance{1, 1};
-  geo[1] = whole ? wgrad_balance_geometry(d_tiles, f_tiles) : WgradBalance{1, 1};
+static void wgrad_balance(const FfnArgs& a, int fh, WgradBalance* geo) {
+  const bool whole = a.d % BN == 0 && !wgrad_small(a.A, a.d, a.f, a.E);
+  geo[0] = whole && fh % BM == 0 ? wgrad_balance_geometry(fh / BM, a.d / BM) : WgradBalance{1, 1};
+  geo[1] = whole && a.f % BM == 0 ? wgrad_balance_geometry(a.d / BM, a.f / BM) : WgradBalance{1, 1};
 }
 
 // The work list both weight-gradient products of a backward call read and (with tokens) the row-tile table
 // of its rows products: one small launch.
-static void launch_bwd_plan(const FfnArgs& a, void* ws, hipStream_t s) {
+void launch_bwd_plan(const FfnArgs& a, int fh, void* ws, hipStream_t s) {
   const int seg_rows_max = wgrad_seg_rows_max(a.A, a.d, a.f, a.E, a.V);
   const int row_blocks = a.A > 0 ? plan_blocks(a) : 0;
   WgradBalance geo[2];
-  wgrad_balance(a, geo);
+  wgrad_balance(a, fh, geo);
   hipLaunchKernelGGL(ffn_bwd_plan_kernel, dim3(1 + row_blocks), dim3(kGemmThreads), 0, s, a.voff, a.owner, a.E, a.V,
                      wgrad_seg_tiles(a.A, a.d, a.f), seg_rows_max,
                      wgrad_plan_at(wgrad_plan_ws(a, ws), seg_rows_max, a.E, a.V, 0),
@@ -422,6 +429,11 @@ static void launch_bwd_plan(const FfnArgs& a, void* ws, hipStream_t s) {
 // Sums of the partial tiles of `n` products (their [M, NC] have the same number of elements).
 static void launch_wgrad_reduce(const FfnArgs& a, const WgradDmaArgs* g, int n, hipStream_t s) {
   if (!g->seg_tiles) return;
+  if (n == 2 && (size_t)g[0].M * g[0].NC != (size_t)g[1].M * g[1].NC) {
+    launch_wgrad_reduce(a, &g[0], 1, s);
+    launch_wgrad_reduce(a, &g[1], 1, s);
+    return;
+  }
   const size_t elems = (size_t)g->M * g->NC;
   const int blocks = (int)std::min<size_t>((elems / 4 + kGemmThreads - 1) / kGemmThreads, 2048);
   const WgradReduceArgs r{(const int4*)g->plan.table, {{g[0].partial, g[0].dw}, {g[n - 1].partial, g[n - 1].dw}}};
@@ -435,17 +447,19 @@ static bool overlap(const void* p, const void* q, size_t bytes_p, size_t bytes_q
 // dXp = dHpre . W1^T (W1_e is [d, f], contraction index f contiguous), dW2 = H^T . dYp, dW1 = Xp^T . dHpre: the weight gradients
 // each with its own partial tiles.  In this order, so that a caller who needs w1, h or dyp no longer may have a gradient written over
 // them: products that share a launch only do where the later one's output is nothing that the earlier one reads.
-static hipError_t launch_bwd_products(const FfnArgs& a, const void* h, const void* dyp, void* dw2, const void* xp, const void* dhpre,
-                                      void* dw1, const void* w1, void* dxp, const int32_t* scatter_src, void* ws, hipStream_t s) {
+// fh: columns of H and rows of dW2 -- a.f, or half of it where dHpre holds two gradients for each of H's columns (gated experts).
+hipError_t launch_bwd_products(const FfnArgs& a, int fh, const void* h, const void* dyp, void* dw2, const void* xp, const void* dhpre,
+                               void* dw1, const void* w1, void* dxp, const int32_t* scatter_src, void* ws, hipStream_t s) {
   void* tail2 = (char*)ws + 2 * align_up((size_t)a.A * a.f * sizeof(bf16_t), 256);
   void* tail1 = (char*)tail2 + wgrad_tail_bytes(a.A, a.d, a.f, a.V);
   unsigned grid[2];
-  const WgradDmaArgs g[2] = {wgrad_dma_args(a, h, dyp, a.f, a.d, dw2, tail2, ws, &grid[0], 0),
+  const WgradDmaArgs g[2] = {wgrad_dma_args(a, h, dyp, fh, a.d, dw2, tail2, ws, &grid[0], 0),
                              wgrad_dma_args(a, xp, dhpre, a.d, a.f, dw1, tail1, ws, &grid[1], 1)};
-  const size_t w_bytes = (size_t)a.E * a.d * a.f * sizeof(bf16_t), row_bytes = (size_t)a.A * sizeof(bf16_t);
-  const bool joint = wgrad_joint(grid[0], grid[1]) && !overlap(dw1, h, w_bytes, row_bytes * a.f) && !overlap(dw1, dyp, w_bytes, row_bytes * a.d);
+  const size_t w_bytes = (size_t)a.E * a.d * a.f * sizeof(bf16_t), w2_bytes = (size_t)a.E * a.d * fh * sizeof(bf16_t);
+  const size_t row_bytes = (size_t)a.A * sizeof(bf16_t);
+  const bool joint = wgrad_joint(grid[0], grid[1]) && !overlap(dw1, h, w_bytes, row_bytes * fh) && !overlap(dw1, dyp, w_bytes, row_bytes * a.d);
   const WgradSmallArgs both{{g[0], g[1]}, grid[0]};
-  if (a.A > 0 && joint && bwd_products_merged(a) && !overlap(dw1, w1, w_bytes, w_bytes) && !overlap(dw2, w1, w_bytes, w_bytes)) {
+  if (a.A > 0 && joint && bwd_products_merged(a) && !overlap(dw1, w1, w_bytes, w_bytes) && !overlap(dw2, w1, w2_bytes, w_bytes)) {
     int bm;
     unsigned rows_grid;
     const SmallArgs p = small_args<EPI_PLAIN>(a, dhpre, w1, nullptr, a.f, a.d, nullptr, dxp, nullptr, ws, nullptr, 1, scatter_src, &bm, &rows_grid);
@@ -474,7 +488,7 @@ static hipError_t launch_bwd_products(const FfnArgs& a, const void* h, const voi
   // (One launch for dXp, dW2 and dW1, which filled the partly empty last rounds of the three grids of 256 x 256 tiles, was measured
   // against three persistent launches: the latter are 2 % faster on the GPT-medium-like backward pass and 4.5 % on the Swin-like one.)
   for (int i = 0; i < 2; ++i) {
-    if (a.f % BM == 0 && a.d % BN == 0)      // whole output tiles: one persistent workgroup per compute unit
+    if (g[i].M % BM == 0 && g[i].NC % BN == 0)      // whole output tiles: one persistent workgroup per compute unit
       hipLaunchKernelGGL(wgrad_gemm_persist_bf16, dim3(std::min(grid[i], (unsigned)kComputeUnits)), dim3(kDmaThreads), 0, s, g[i]);
     else
       hipLaunchKernelGGL(wgrad_gemm_dma_bf16, dim3(grid[i]), dim3(kDmaThreads), 0, s, g[i]);
@@ -522,6 +536,10 @@ hipError_t launch_ffn_fwd_top1_bf16(const FfnArgs& a, const void* x, const int32
   return launch_rows<false, EPI_PLAIN>(a, h, w2, b2, a.f, a.d, nullptr, y, nullptr, ws, s, nullptr, 1, rows_split_ws(a, ws), src);
 }
 
+hipError_t launch_rows_plain(const FfnArgs& a, const void* in, const void* w, const void* bias, int K, void* out, void* ws, hipStream_t s) {
+  return launch_rows<false, EPI_PLAIN>(a, in, w, bias, K, a.d, nullptr, out, nullptr, ws, s, nullptr, 1, rows_split_ws(a, ws));
+}
+
 // scatter_src (top-1 layers, needs f % 128 == 0): bucket row p of dXp is stored as row scatter_src[p] of
 // `dxp`, which is then dX [N, d] itself -- the backward reverse routing folded into the epilogue.
 // h_kept: act(Hpre) as the forward pass left it in the caller's buffer, or null: it is computed again from
@@ -533,14 +551,14 @@ hipError_t launch_ffn_bwd_bf16(const FfnArgs& a, const void* dyp, const void* xp
   bf16_t* h_ws = (bf16_t*)((char*)ws + align_up((size_t)a.A * a.f * sizeof(bf16_t), 256));
   const bf16_t* h = h_kept ? (const bf16_t*)h_kept : h_ws;
   hipError_t err;
-  launch_bwd_plan(a, ws, s);
+  launch_bwd_plan(a, a.f, ws, s);
   if (a.A > 0) {
     // dH = dYp . W2^T fused with act'(Hpre); W2_e is [f, d], contraction index d contiguous
     err = h_kept ? launch_rows<true, EPI_DHQ>(a, dyp, w2, nullptr, a.d, a.f, hpre, dhpre, nullptr, ws, s)
                  : launch_rows<true, EPI_DH>(a, dyp, w2, nullptr, a.d, a.f, hpre, dhpre, h_ws, ws, s);
     if (err != hipSuccess) return err;
   }
-  return launch_bwd_products(a, h, dyp, dw2, xp, dhpre, dw1, w1, dxp, scatter_src, ws, s);
+  return launch_bwd_products(a, a.f, h, dyp, dw2, xp, dhpre, dw1, w1, dxp, scatter_src, ws, s);
 }
 
 }  // namespace flexmoe
@@ -558,7 +576,7 @@ extern "C" void flexmoe_debug_bf16_paths(int A, int d, int f, int E, int V, long
   wgrad_dma_args(a, nullptr, nullptr, d, f, nullptr, nullptr, nullptr, &grid[1], 1);
   const bool joint = small && wgrad_joint(grid[0], grid[1]);
   WgradBalance geo[2];
-  wgrad_balance(a, geo);
+  wgrad_balance(a, f, geo);
   out[0] = small_rows(A, d, f, E, V);
   out[1] = small;
   out[2] = joint;

@@ -1,6 +1,8 @@
 // Direct-to-LDS pipeline (global_load_lds): operand sources, the K loop in its one-tile and its continuing form, the sum of the split last round.
-// Part of the bf16 expert-FFN kernels; included by ffn_bf16.hip only (one translation unit).
+// Part of the expert-FFN kernels: ffn_bf16.hip, ffn_gated.hip and ffn_i8.hip include it.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 #include "ffn_bf16_tile.h"
 namespace flexmoe {
@@ -153,13 +155,21 @@ template <int TILES> __device__ __forceinline__ void wait_tiles_in_flight() { wa
 // tile holds row L % 16 and the four consecutive columns 4 (L / 16) ..: acc[i][j][2 si + sj] is the tile of rows
 // 16 si .., columns 16 sj .. of the wave's 32-row block i and 32-column block j.
 typedef f32x16 DmaAcc[MB][NBW];      // [i][j], elements 4 (2 si + sj) .. + 3: one 16 x 16 tile each
-__device__ __forceinline__ void zero_acc(DmaAcc& acc) {
+// (8-bit integer operands: v_mfma_i32_16x16x64_i8 with sums in int32, the same bytes in the same lanes -- a 64-byte K
+// tile row is 32 bf16 or 64 integers -- so the loads, the LDS tiles and the loop are the same; the accumulators' type
+// says which it is.)
+typedef i32x16 DmaAccI8[MB][NBW];
+template <typename T> __device__ __forceinline__ void zero_acc(T (&acc)[MB][NBW]) {
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NBW; ++j)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+}
+__device__ __forceinline__ f32x4 mma_16x16(bf16x8 b, bf16x8 a, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0); }
+__device__ __forceinline__ i32x4 mma_16x16(bf16x8 b, bf16x8 a, i32x4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a), c, 0, 0, 0);
 }
 // A K tile is multiplied in two halves: row blocks 0, 1 of the wave (a0: four 16-row fragments), then 2, 3 (a1),
 // each against all four 16-column fragments b, which are read once per tile.
@@ -201,15 +211,15 @@ __device__ __forceinline__ void dma_read_first(DmaFrags& f, const lds_byte_t* st
 // PRIO: the wave runs its four instructions at raised priority (the SIMD's other wave then gets its loads and LDS
 // reads in behind them instead of between them).  Measured on the GPT-XL-like layer: backward products -0.4 ... -0.7 %,
 // forward products (one operand read with transposing loads) +0.3 %, so only the former ask for it.
-template <bool PRIO>
-__device__ __forceinline__ void dma_mfma_group(DmaAcc& acc, const Frag8 (&a)[4], const Frag8& b, int half, int q) {
+template <bool PRIO, typename T>
+__device__ __forceinline__ void dma_mfma_group(T (&acc)[MB][NBW], const Frag8 (&a)[4], const Frag8& b, int half, int q) {
   if (PRIO) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    f32x16& t = acc[2 * half + (p >> 1)][q >> 1];
+    T& t = acc[2 * half + (p >> 1)][q >> 1];
     const int e = 4 * (2 * (p & 1) + (q & 1));
-    f32x4 c = {t[e], t[e + 1], t[e + 2], t[e + 3]};
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v, a[p].v, c, 0, 0, 0);
+    typename std::conditional<std::is_same<T, f32x16>::value, f32x4, i32x4>::type c = {t[e], t[e + 1], t[e + 2], t[e + 3]};
+    c = mma_16x16(b.v, a[p].v, c);
     t[e] = c[0];
     t[e + 1] = c[1];
     t[e + 2] = c[2];
@@ -235,8 +245,8 @@ __device__ __forceinline__ void dma_mfma_group(DmaAcc& acc, const Frag8 (&a)[4],
 // part of tile kt+1 has landed.
 // `issue` serves the first half of the step (PRE), `issue_post` the second (POST): the same object inside a
 // tile sequence, two different ones where the sequence of the workgroup's next output tile takes over.
-template <bool TRA, bool TRB, bool PRE, bool POST, int WAIT, bool NEXT, typename Issue, typename IssuePost>
-__device__ __forceinline__ void dma_step(lds_byte_t* prev, lds_byte_t* cur, const lds_byte_t* nxt, DmaAcc& acc,
+template <bool TRA, bool TRB, bool PRE, bool POST, int WAIT, bool NEXT, typename T, typename Issue, typename IssuePost>
+__device__ __forceinline__ void dma_step(lds_byte_t* prev, lds_byte_t* cur, const lds_byte_t* nxt, T (&acc)[MB][NBW],
                                          DmaFrags& f, Issue& issue, IssuePost& issue_post, int wm, int cb0) {
   constexpr int kEvery = 4 / kOpLoads;      // a load after every kEvery-th group of four MFMAs
   // (behind an empty asm: each fragment address is derived from these where it is used, not once for the whole loop)
@@ -326,9 +336,9 @@ template <typename Issue> __device__ __forceinline__ void dma_prefetch3(lds_byte
 // make_next(next) builds the next tile's sequence; it is called behind the steady-state loop, so that the
 // sequence's registers are not live across it (spilled registers come back through the same in-order
 // queue as the operand tiles: every reload inside the K loop would wait for all tiles in flight).
-template <bool TRA, bool TRB, typename Issue, typename After, typename MakeNext>
+template <bool TRA, bool TRB, typename T, typename Issue, typename After, typename MakeNext>
 __device__ __forceinline__ void dma_pipeline_cont(lds_byte_t* s0, lds_byte_t* s1, lds_byte_t* s2, lds_byte_t* s3,
-                                                  DmaAcc& acc, Issue& issue, int KT, Issue& next, int wm,
+                                                  T (&acc)[MB][NBW], Issue& issue, int KT, Issue& next, int wm,
                                                   int cb0, After after_barrier, MakeNext make_next) {
   wait_tiles_in_flight<2>();                           // tile 0 has landed
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -375,7 +385,7 @@ struct RowsDmaArgs {
 // Sum of the K segments of the split tail tiles (see lookup_row_tile): out = bf16(sum over
 // segments in order + bias).  Grid: (kSplitSlices row slices of a tile, kSplitUnits / 2 tail tiles at most).
 constexpr int kSplitSlices = 16;
-__global__ __launch_bounds__(kGemmThreads) void rows_split_reduce_kernel(const RowsDmaArgs p) {
+static __global__ __launch_bounds__(kGemmThreads) void rows_split_reduce_kernel(const RowsDmaArgs p) {
   __shared__ int s_tile[8];
   RowTile t;
   const SplitArg sp{p.normal_grid, p.K / DK, (int)blockIdx.y};

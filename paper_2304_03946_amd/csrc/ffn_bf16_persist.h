@@ -1,6 +1,6 @@
 // Persistent rows kernels: one workgroup per compute unit walks its share of the output tiles, and the
 // operand loads of a tile's successor are issued while the tile's own K loop drains.
-// Part of the bf16 expert-FFN kernels; included by ffn_bf16.hip only (one translation unit).
+// Part of the expert-FFN kernels: ffn_bf16.hip, ffn_gated.hip and ffn_i8.hip include it.
 #pragma once
 #include "common.h"
 #include "ffn_bf16_tile.h"
@@ -22,7 +22,6 @@ namespace flexmoe {
 // the grid and their S x tail_tiles K segments form one more round, workgroup b taking segment
 // (b % S) of tail tile b / S.
 // =============================================================================================
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef const i32x4 __attribute__((address_space(4)))* RowTabPtr;
 
 // tab[0] = {row tiles of the bucket list, 0, 0, 0}; tab[1 + t] = {first row, rows, expert, 0} of row tile t.
@@ -67,9 +66,9 @@ __device__ __forceinline__ void rows_plan_block(const int32_t* __restrict__ voff
   }
 }
 
-__global__ __launch_bounds__(kGemmThreads) void rows_plan_kernel(const int32_t* __restrict__ voff,
-                                                                 const int32_t* __restrict__ owner, int V,
-                                                                 i32x4* __restrict__ tab) {
+static __global__ __launch_bounds__(kGemmThreads) void rows_plan_kernel(const int32_t* __restrict__ voff,
+                                                                        const int32_t* __restrict__ owner, int V,
+                                                                        i32x4* __restrict__ tab) {
   rows_plan_block(voff, owner, V, tab, blockIdx.x, gridDim.x);
 }
 

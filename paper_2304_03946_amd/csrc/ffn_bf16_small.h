@@ -1,5 +1,5 @@
 // Rows GEMMs for buckets that do not fill 256-row tiles: decode steps, short prompts, small training batches, many
-// small experts.  Part of the bf16 expert-FFN kernels; included by ffn_bf16.hip only (one translation unit).
+// small experts.  Part of the expert-FFN kernels: ffn_bf16.hip, ffn_gated.hip and ffn_i8.hip include it.
 #pragma once
 #include "common.h"
 #include "ffn_bf16_tile.h"
@@ -168,8 +168,8 @@ __device__ __forceinline__ void small_plan_block(const int32_t* __restrict__ vof
     for (int i = w % plan.parts * kWave + lane; i < len; i += plan.parts * kWave) plan.rowmap[to + i] = lo + i;
   }
 }
-__global__ __launch_bounds__(kGemmThreads) void small_plan_kernel(const int32_t* __restrict__ voff,
-                                                                  const int32_t* __restrict__ owner, int E, int V, SmallPlan plan) {
+static __global__ __launch_bounds__(kGemmThreads) void small_plan_kernel(const int32_t* __restrict__ voff,
+                                                                         const int32_t* __restrict__ owner, int E, int V, SmallPlan plan) {
   small_plan_block(voff, owner, E, V, plan, blockIdx.x, gridDim.x);
 }
 

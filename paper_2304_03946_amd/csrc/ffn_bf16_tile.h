@@ -1,5 +1,5 @@
 // Tile mapping, register-staged operand loads, LDS -> MFMA fragments, activation tables, epilogues and the register-staged rows kernel.
-// Part of the bf16 expert-FFN kernels; included by ffn_bf16.hip only (one translation unit).
+// Part of the expert-FFN kernels: ffn_bf16.hip, ffn_gated.hip and ffn_i8.hip include it.
 #pragma once
 #include "common.h"
 

@@ -75,8 +75,8 @@ template <bool KC, int W> struct F32Op {
 typedef f32x4 F32Acc[2][2];                          // a wave's 32 x 32 outputs: 16-row and 16-column blocks
 
 // A workgroup's K loop: MT 32-row blocks x 64 columns.  MT == 2: a wave per 32 x 32 outputs.  MT == 1: two waves per 32 x 32 outputs,
-// one for the even K tiles, one for the odd ones.  A stage holds 3 - MT K tiles.
-template <int MT, bool KC0, bool KC1> struct F32Loop {
+// one for the even K tiles, one for the odd ones.  A stage holds 3 - MT K tiles.  BY_ROWS: see run.
+template <int MT, bool KC0, bool KC1, bool BY_ROWS = false> struct F32Loop {
   typedef F32Op<KC0, MT * 32> Op0;
   typedef F32Op<KC1, FN> Op1;
   static constexpr int kSub = 3 - MT;                // K tiles of a stage
@@ -123,7 +123,7 @@ template <int MT, bool KC0, bool KC1> struct F32Loop {
 
   // KT stages; issue(s, lds address) starts the wave's loads of one.
   // acc[i][j]: row 16 i + lane % 16, columns 16 j + 4 (lane / 16) .. of the wave's block.  MT == 1: on return the wave with the even K tiles
-  // has the sums of the block's first 16 columns, the other one of the rest.
+  // has the sums of the block's first 16 columns, the other one of the rest (BY_ROWS: of its first 16 rows, and of the rest).
   // Either way a sum is that of the even K tiles, ascending, plus that of the odd ones: MT == 2 keeps the two in accumulators of their own.
   template <typename Issue>
   static __device__ __forceinline__ void run(lds_t* sm, F32Acc& acc, int KT, Issue issue) {
@@ -168,15 +168,20 @@ template <int MT, bool KC0, bool KC1> struct F32Loop {
       const int keep = wave >> 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const f32x4 first = acc[i][0], second = acc[i][1];
+        const f32x4 first = BY_ROWS ? acc[0][i] : acc[i][0], second = BY_ROWS ? acc[1][i] : acc[i][1];
         *(Ptr)(sm + ((wave * 2 + i) * kWave + lane) * 16) = keep ? first : second;
       }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const f32x4 v = *(Ptr)(sm + (((wave ^ 2) * 2 + i) * kWave + lane) * 16);      // (even K tiles + odd ones, in either wave)
-        acc[i][0] += v;
-        acc[i][1] += v;
+        if (BY_ROWS) {
+          acc[0][i] += v;
+          acc[1][i] += v;
+        } else {
+          acc[i][0] += v;
+          acc[i][1] += v;
+        }
       }
     }
   }
@@ -326,6 +331,130 @@ __global__ __launch_bounds__(kF32Threads, 2) void rows_gemm_f32(const float* __r
       *(float4*)(out0 + o) = make_float4(c[0] * act_deriv(z.x, act), c[1] * act_deriv(z.y, act), c[2] * act_deriv(z.z, act),
                                          c[3] * act_deriv(z.w, act));
       if (out1) *(float4*)(out1 + o) = make_float4(act_apply(z.x, act), act_apply(z.y, act), act_apply(z.z, act), act_apply(z.w, act));
+    }
+  }
+}
+
+// The two products of gated experts that have an activation (H = act(G) * U; G, U, dG and dU are the halves of Hpre and dHpre [A, 2 f]).
+// EPI_FWD1: [G, U] = In . W1_e + b1_e, W1_e [K, 2 f]; a tile's 64 columns are 32 of G and the same 32 of U, 16 and 16 in turn, so that a
+// wave's blocks j = 0 and 1 are G and U of the same outputs.  EPI_DH: dH = In . W2_e^T, W2_e [f, K], in 64 columns; dG = dH * U * act'(G),
+// dU = dH * act(G).
+__device__ __forceinline__ void gate_f32(float z, int act, float* a, float* da) {
+  if (act == FLEXMOE_SILU) {
+    const float s = 1.f / (1.f + expf(-z));
+    *a = z * s;
+    *da = s * (1.f + z * (1.f - s));
+  } else {
+    *a = act_apply(z, act);
+    *da = act_deriv(z, act);
+  }
+}
+template <int MT, int EPI>
+__global__ __launch_bounds__(kF32Threads, 2) void rows_gated_f32(const float* __restrict__ in, const float* __restrict__ w,
+                                                                 const float* __restrict__ bias, const int32_t* __restrict__ voff,
+                                                                 const int32_t* __restrict__ owner, int V, int K, int f, int ct0,
+                                                                 int col_tiles, int act, const float* __restrict__ hpre_in,
+                                                                 float* __restrict__ out0, float* __restrict__ out1) {
+  constexpr bool FWD = EPI == EPI_FWD1;
+  typedef F32Loop<MT, true, !FWD, FWD> Loop;
+  __shared__ __align__(1024) unsigned char smem[Loop::kLds];
+  __shared__ int s_tile[4];
+  int row0, rows, e, ct;
+  if (!f32_tile<MT * 32>(voff, owner, V, col_tiles, s_tile, &row0, &rows, &e, &ct)) return;
+  const int n0 = (ct0 + ct) * (FWD ? FN / 2 : FN), cols = min(FWD ? FN / 2 : FN, f - n0);
+  const float* we = w + (size_t)e * K * (FWD ? 2 * f : f);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+
+  const float* const a_base = in + (size_t)row0 * K;
+  const float* const w_base = we + (FWD ? (size_t)n0 : (size_t)n0 * K);
+  size_t aoff[Loop::kL0], woff[Loop::kL1];
+  int ak[Loop::kL0], wk[Loop::kL1];
+#pragma unroll
+  for (int q = 0; q < Loop::kL0; ++q) {
+    const int i = Loop::piece0(wave, q);
+    ak[q] = Loop::sub0(wave, q) * FK + Loop::Op0::k(i, lane);
+    aoff[q] = (uint64_t)(uint32_t)min(Loop::Op0::out(i, lane), rows - 1) * (uint32_t)K + ak[q];
+  }
+#pragma unroll
+  for (int q = 0; q < Loop::kL1; ++q) {
+    const int i = Loop::piece1(wave, q), o = Loop::Op1::out(i, lane);
+    wk[q] = Loop::sub1(wave, q) * FK + Loop::Op1::k(i, lane);
+    woff[q] = FWD ? (uint64_t)(uint32_t)wk[q] * (2u * (uint32_t)f) + min((o >> 5) * 16 + (o & 15), cols - 4) + (o & 16 ? f : 0)
+                  : (uint64_t)(uint32_t)min(o, cols - 1) * (uint32_t)K + wk[q];
+  }
+  constexpr int kStep = Loop::kSub * FK;
+  auto issue = [&](int s, unsigned lds) {
+    const int k0 = s * kStep;
+    const float *ab = a_base + k0, *wb = w_base + (FWD ? (size_t)k0 * 2 * f : (size_t)k0);
+    if (k0 + kStep <= K) {
+#pragma unroll
+      for (int q = 0; q < Loop::kL0; ++q) f32_load(ab + aoff[q], lds + Loop::dst0(wave, q));
+#pragma unroll
+      for (int q = 0; q < Loop::kL1; ++q) f32_load(wb + woff[q], lds + Loop::dst1(wave, q));
+    } else {                                         // past K: zeros
+#pragma unroll
+      for (int q = 0; q < Loop::kL0; ++q) f32_load(k0 + ak[q] < K ? ab + aoff[q] : (const float*)&kF32Zero, lds + Loop::dst0(wave, q));
+#pragma unroll
+      for (int q = 0; q < Loop::kL1; ++q) f32_load(k0 + wk[q] < K ? wb + woff[q] : (const float*)&kF32Zero, lds + Loop::dst1(wave, q));
+    }
+  };
+  F32Acc acc;
+  Loop::run((lds_t*)smem, acc, (K + kStep - 1) / kStep, issue);
+
+  auto row_at = [&](int i) { return (MT == 2 ? (wave >> 1) * 32 : 0) + i * 16 + (lane & 15); };
+  if (FWD) {
+    const int col = n0 + (wave & 1) * 16 + 4 * (lane >> 4);
+    if (col >= f) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (row_at(i) >= rows || (MT == 1 && i != (wave >> 1))) continue;
+      const size_t row = row0 + row_at(i);
+      f32x4 g = acc[i][0], u = acc[i][1], h;
+      if (bias) {
+        g += *(const f32x4*)(bias + (size_t)e * 2 * f + col);
+        u += *(const f32x4*)(bias + (size_t)e * 2 * f + f + col);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float a, da;
+        gate_f32(g[q], act, &a, &da);
+        h[q] = a * u[q];
+      }
+      if (out0) {
+        *(f32x4*)(out0 + row * 2 * f + col) = g;
+        *(f32x4*)(out0 + row * 2 * f + f + col) = u;
+      }
+      *(f32x4*)(out1 + row * f + col) = h;
+    }
+  } else {
+    auto col_at = [&](int j) { return n0 + (wave & 1) * 32 + j * 16 + 4 * (lane >> 4); };
+    auto stored = [&](int x) { return row_at(x >> 1) < rows && col_at(x & 1) < f && (MT == 2 || (x & 1) == (wave >> 1)); };
+    f32x4 zg[4], zu[4];                              // (one trip to memory, not one after another)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (stored(x)) {
+        const float* at = hpre_in + (size_t)(row0 + row_at(x >> 1)) * 2 * f + col_at(x & 1);
+        zg[x] = *(const f32x4*)at;
+        zu[x] = *(const f32x4*)(at + f);
+      }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (!stored(x)) continue;
+      const size_t row = row0 + row_at(x >> 1);
+      const int col = col_at(x & 1);
+      f32x4 dg, du, h;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float dh = acc[x >> 1][x & 1][q];
+        float a, da;
+        gate_f32(zg[x][q], act, &a, &da);
+        dg[q] = dh * zu[x][q] * da;
+        du[q] = dh * a;
+        h[q] = a * zu[x][q];
+      }
+      *(f32x4*)(out0 + row * 2 * f + col) = dg;
+      *(f32x4*)(out0 + row * 2 * f + f + col) = du;
+      if (out1) *(f32x4*)(out1 + row * f + col) = h;
     }
   }
 }
@@ -501,6 +630,26 @@ static void launch_rows_f32(const FfnArgs& a, const void* in, const void* w, con
   }
 }
 
+// a.f: columns of H
+template <int EPI>
+static void launch_gated_f32(const FfnArgs& a, const void* in, const void* w, const void* bias, const void* hpre_in, void* out0, void* out1,
+                             hipStream_t s) {
+  constexpr int kCols = EPI == EPI_FWD1 ? FN / 2 : FN;
+  const int mt = f32_rows_blocks(a, a.d, EPI == EPI_FWD1 ? 2 * a.f : a.f), cols = (int)tiles_of(a.f, kCols);
+  const long long row_tiles = a.A / (mt * 32) + a.V;
+  const int most = (int)std::max((((1ll << 32) / kF32Threads - 1) / kF32Xcds * kF32Xcds) / row_tiles, 1ll);      // as launch_rows_f32
+  for (int ct0 = 0; ct0 < cols; ct0 += most) {
+    const int n = std::min(most, cols - ct0);
+    const dim3 grid((unsigned)((row_tiles * n + kF32Xcds - 1) / kF32Xcds * kF32Xcds));
+    if (mt == 2)
+      hipLaunchKernelGGL((rows_gated_f32<2, EPI>), grid, dim3(kF32Threads), 0, s, (const float*)in, (const float*)w, (const float*)bias,
+                         a.voff, a.owner, a.V, a.d, a.f, ct0, n, a.act, (const float*)hpre_in, (float*)out0, (float*)out1);
+    else
+      hipLaunchKernelGGL((rows_gated_f32<1, EPI>), grid, dim3(kF32Threads), 0, s, (const float*)in, (const float*)w, (const float*)bias,
+                         a.voff, a.owner, a.V, a.d, a.f, ct0, n, a.act, (const float*)hpre_in, (float*)out0, (float*)out1);
+  }
+}
+
 static void launch_wgrad_f32(const FfnArgs& a, const void* L, const void* R, int M, int NC, void* dw, hipStream_t s) {
   const int mt = f32_wgrad_blocks(a, M, NC);
   // a grid's second dimension ends at 65535 workgroups: layers of millions of columns take several launches
@@ -536,6 +685,28 @@ hipError_t launch_ffn_bwd_f32(const FfnArgs& a, const void* dyp, const void* xp,
   const float* h = h_kept ? (const float*)h_kept : h_ws;
   launch_wgrad_f32(a, h, dyp, a.f, a.d, dw2, s);
   launch_wgrad_f32(a, xp, dhpre, a.d, a.f, dw1, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_ffn_gated_fwd_f32(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
+                                    void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s) {
+  if (a.A == 0) return hipSuccess;
+  void* h = h_keep ? h_keep : ws;
+  launch_gated_f32<EPI_FWD1>(a, xp, w1, b1, nullptr, hpre, h, s);
+  launch_rows_f32<false, EPI_PLAIN>(a, h, w2, b2, a.f, a.d, nullptr, yp, nullptr, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_ffn_gated_bwd_f32(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept, const void* w1,
+                                    const void* w2, void* dxp, void* dw1, void* dw2, void* ws, hipStream_t s) {
+  float* dhpre = (float*)ws;
+  float* h_ws = (float*)((char*)ws + align_up((size_t)a.A * 2 * a.f * sizeof(float), 256));
+  if (a.A > 0) {
+    launch_gated_f32<EPI_DH>(a, dyp, w2, nullptr, hpre, dhpre, h_kept ? nullptr : h_ws, s);
+    launch_rows_f32<true, EPI_PLAIN>(a, dhpre, w1, nullptr, 2 * a.f, a.d, nullptr, dxp, nullptr, s);
+  }
+  launch_wgrad_f32(a, h_kept ? (const float*)h_kept : h_ws, dyp, a.f, a.d, dw2, s);
+  launch_wgrad_f32(a, xp, dhpre, a.d, 2 * a.f, dw1, s);
   return hipGetLastError();
 }
 

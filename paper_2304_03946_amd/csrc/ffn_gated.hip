@@ -1,0 +1,548 @@
+// Gated expert FFN per vExpert bucket in bf16, forward and backward, as grouped GEMMs on the matrix cores (fp32 sums):
+//   G = X Wg + bg,  U = X Wu + bu        one product with W1 = [Wg, Wu] [d, 2 f]; Hpre = [G, U] [A, 2 f] is kept for the backward pass
+//   H = act(G) * U                        in that product's epilogue, from the fp32 sums
+//   Y = H W2 + b2
+// and for an upstream gradient dY
+//   dH = dY W2^T;   dG = dH * U * act'(G),  dU = dH * act(G)      the epilogue of dH's product; dHpre = [dG, dU]
+//   dX = dHpre W1^T,  dW1 = X^T dHpre,  dW2 = H^T dY
+//
+// The products without an activation -- Y, dX, dW1, dW2 -- are those of an ungated layer with 2 f (W1) or f (W2) columns in the middle,
+// on the kernels of ffn_bf16.hip.  The two with one have kernels here, on the same loops:
+//  * a tile of the first product holds a column of G and the same column of U in the same lane: its weight columns are taken from the two
+//    halves of W1 in turn, 32 and 32 (16 and 16 in the few-rows kernels).  Only the addresses of the weights' loads know about it.
+//  * G, U and H leave through a wave-private LDS patch as bf16 (half of what fp32 patches move): 16 bytes per lane, 64 per row.
+//  * three sets of kernels, chosen as for an ungated layer with 2 f columns: rows of 256 x 256 tiles with direct-to-LDS loads where K is a
+//    multiple of 128, register-staged ones for other K, and 32- or 64-row tiles for few rows (small_core).
+// Rounding: H is made of the sums before G and U are rounded to bf16 for Hpre (an error of 2^-9 each that y then does not have);
+// the backward pass has only the rounded ones, for act', act and, unless the caller kept H, for H.
+//
+// What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.
+#include <algorithm>
+
+#include "common.h"
+#include "ffn_bf16_host.h"
+#include "ffn_bf16_tile.h"
+#include "ffn_bf16_dma.h"
+#include "ffn_bf16_persist.h"
+#include "ffn_bf16_small.h"
+#include "ffn_small_core.h"
+
+namespace flexmoe {
+
+// act(z) and act'(z); SiLU z s with s = 1 / (1 + e^-z): exp2 and reciprocal of the hardware, 1 ulp each
+template <int ACT> __device__ __forceinline__ void gate_act(float z, float* a, float* da) {
+  if (ACT == FLEXMOE_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
+    *a = z * s;
+    *da = fmaf(*a, 1.f - s, s);
+  } else {
+    act_both<ACT>(z, a, da);
+  }
+}
+
+struct GatedArgs {
+  const bf16_t* in;              // fwd: Xp, dH: dYp
+  const bf16_t* w;               // fwd: W1 [E, d, 2 f], dH: W2 [E, f, d]
+  const bf16_t* bias;            // [E, 2 f] or null (fwd)
+  const int32_t* voff;
+  const int32_t* owner;
+  int V, K, f, row_tiles_max, col_tiles;
+  const bf16_t* hpre_in;         // dH: Hpre [A, 2 f]
+  bf16_t* out0;                  // fwd: Hpre or null, dH: dHpre [A, 2 f]
+  bf16_t* out1;                  // fwd: H [A, f], dH: H or null (kept by the forward pass)
+  int act;
+};
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void store_nt16(void* p, u32x4_t v) { __builtin_nontemporal_store(v, (u32x4_t*)p); }
+
+// Columns of a 256-column tile that the first product takes from either half of W1.
+constexpr int GN = BN / 2;
+
+// The weights' loads of the first product: DmaSrcT with tile column 32 b + c taken from column n0 + 32 (b / 2) + c of half b % 2.
+struct DmaSrcGate {
+  DmaSrcT s;
+  __device__ __forceinline__ void init(const bf16_t* b, int f, int cols_valid) {
+    s.base = b;
+    s.ld = 2 * (size_t)f;
+    const int tid = opaque_tid();
+    const int w = tid >> 6, i = tid & 63;
+#pragma unroll
+    for (int q = 0; q < kOpLoads; ++q) {
+      const int krow = (w * kOpLoads + q) * 2 + (i >> 5);
+      const int c = dmat_chunk(krow, i & 31);
+      const int in_half = min((c >> 3) * 4 + (c & 3), cols_valid / 8 - 1);
+      s.off[q] = (uint32_t)((uint32_t)krow * 2u * (uint32_t)f + (uint32_t)in_half * 8u + ((c >> 2) & 1 ? (uint32_t)f : 0u)) * 2u;
+    }
+  }
+  __device__ __forceinline__ void part(lds_byte_t* tile, int k0, int q) const { s.part(tile, k0, q); }
+};
+
+// ---- epilogues of the 256 x 256 kernels --------------------------------------------------------
+// Forward.  The wave's accumulators acc[i][0] (G) and acc[i][1] (U) hold 128 rows x 32 columns, 16 x 16 tiles [2 si + sj]: lane L has row
+// 16 si + L % 16, columns 16 sj + 4 (L / 16) .. .  16 rows at a time go through the patch: three [16][32] bf16 tiles (64-byte rows, chunk
+// index XOR row / 4: writes and reads free of bank conflicts), read back as 16 bytes per lane.
+template <int ACT, bool FULL>
+__device__ __forceinline__ void gated_fwd_rounds(lds_byte_t* patch, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wm, int c0) {
+  const int lane = opaque_tid() & 63;
+  const int r = lane & 15, g4 = lane >> 4;
+  const int f = p.f;
+  float bg[2][4] = {}, bu[2][4] = {};
+  if (p.bias) {
+    const bf16_t* b = p.bias + (size_t)t.e * 2 * f;
+#pragma unroll
+    for (int sj = 0; sj < 2; ++sj) {
+      const int col = min(c0 + 16 * sj + 4 * g4, f - 4);
+      unpack4(*(const uint2*)(b + col), bg[sj]);
+      unpack4(*(const uint2*)(b + f + col), bu[sj]);
+    }
+  }
+  // what the lane stores: 16 bytes of row `lane / 4` of the 16
+  const int srow = lane >> 2, ch = lane & 3;
+  const uint32_t read_at = srow * 64 + ((ch ^ (srow >> 2)) << 4);
+  const int col = c0 + ch * 8;
+  const bool col_ok = FULL || col < f;
+  bf16_t* const pre_t = p.out0 ? p.out0 + (size_t)t.row0 * 2 * f + col : nullptr;
+  bf16_t* const h_t = p.out1 + (size_t)t.row0 * f + col;
+  const uint32_t row_first = wm * 32 + srow;             // of the tile, round (0, 0)
+#pragma unroll
+  for (int round = 0; round < 2 * MB; ++round) {
+    const int i = round >> 1, sub = round & 1;
+#pragma unroll
+    for (int sj = 0; sj < 2; ++sj) {
+      const int e = 4 * (2 * sub + sj);
+      float g[4], u[4], h[4], da;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        g[q] = acc[i][0][e + q] + bg[sj][q];
+        u[q] = acc[i][1][e + q] + bu[sj][q];
+        gate_act<ACT>(g[q], &h[q], &da);
+        h[q] *= u[q];
+      }
+      const uint32_t at = r * 64 + (((sj * 2 + (g4 >> 1)) ^ (r >> 2)) << 4) + (g4 & 1) * 8;
+      typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
+      *(lds_u32x2*)(patch + at) = u32x2_t{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])};
+      *(lds_u32x2*)(patch + 1024 + at) = u32x2_t{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3])};
+      *(lds_u32x2*)(patch + 2048 + at) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+    }
+    asm volatile("" ::: "memory");                       // (a wave's LDS instructions execute in order)
+    typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4;
+    const u32x4_t vg = *(lds_u32x4*)(patch + read_at), vu = *(lds_u32x4*)(patch + 1024 + read_at), vh = *(lds_u32x4*)(patch + 2048 + read_at);
+    asm volatile("" ::: "memory");
+    const uint32_t row = row_first + i * 64 + sub * 16;
+    if (FULL || (col_ok && (int)row < t.rows_valid)) {
+      if (pre_t) {
+        bf16_t* o = pre_t + (size_t)row * 2 * f;
+        store_nt16(o, vg);
+        store_nt16(o + f, vu);
+      }
+      store_nt16(h_t + (size_t)row * f, vh);
+    }
+  }
+}
+
+// dH: the wave's accumulators are 128 rows x 64 columns of dH, rounds and fp32 patch as in epilogue_rounds8.  The side inputs G and U are
+// requested a round ahead.
+template <int ACT, bool KEPT, bool FULL>
+__device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wm, int col_base) {
+  const int lane = opaque_tid() & 63;
+  const int rsub = lane >> 4, c = lane & 15;
+  const int f = p.f;
+  constexpr int kRounds = MB * 2, kIts = 4, kAhead = 1;
+  const int col = col_base + jh * 64 + c * 4;            // of H
+  const bool col_ok = FULL || col < f;
+  const size_t tile_at = (size_t)t.row0 * 2 * f + col;
+  const bf16_t* const pre_t = p.hpre_in + tile_at;
+  bf16_t* const dpre_t = p.out0 + tile_at;
+  bf16_t* const h_t = KEPT ? nullptr : p.out1 + (size_t)t.row0 * f + col;
+  auto row_of = [&](int round, int it) { return (wm + 2 * (round >> 1)) * 32 + (round & 1) * 16 + it * 4 + rsub; };
+  uint2 sg[kAhead + 1][kIts], su[kAhead + 1][kIts];
+  auto fetch_round = [&](int round) {
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const int row = row_of(round, it);
+      uint2 g = make_uint2(0, 0), u = make_uint2(0, 0);
+      if (FULL || (col_ok && row < t.rows_valid)) {
+        const bf16_t* at = pre_t + (size_t)((uint32_t)row * 2u) * f;
+        g = *(const uint2*)at;
+        u = *(const uint2*)(at + f);
+      }
+      sg[round % (kAhead + 1)][it] = g;
+      su[round % (kAhead + 1)][it] = u;
+    }
+  };
+  auto write_round = [&](int i, int sub) {
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int sj = 0; sj < 2; ++sj) {
+        const int cc = jj * 8 + sj * 4 + rsub;
+        const f32x16& a = acc[i][jj];
+        const int e = 4 * (2 * sub + sj);
+        *(float4*)(patch + c * 64 + ((cc ^ c) << 2)) = make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
+      }
+  };
+#pragma unroll
+  for (int round = 0; round < kAhead; ++round) fetch_round(round);
+  write_round(0, 0);
+#pragma unroll
+  for (int round = 0; round < kRounds; ++round) {
+    if (round + kAhead < kRounds) fetch_round(round + kAhead);
+    asm volatile("" ::: "memory");
+    float4 v[kIts];
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const int row = it * 4 + rsub;
+      v[it] = *(const float4*)(patch + row * 64 + ((c ^ row) << 2));
+    }
+    asm volatile("" ::: "memory");
+    if (round + 1 < kRounds) write_round((round + 1) >> 1, (round + 1) & 1);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      float g[4], u[4], dh[4] = {v[it].x, v[it].y, v[it].z, v[it].w}, dg[4], du[4], h[4];
+      unpack4(sg[round % (kAhead + 1)][it], g);
+      unpack4(su[round % (kAhead + 1)][it], u);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float a, da;
+        gate_act<ACT>(g[q], &a, &da);
+        dg[q] = dh[q] * u[q] * da;
+        du[q] = dh[q] * a;
+        h[q] = a * u[q];
+      }
+      const int row = row_of(round, it);
+      if (FULL || (col_ok && row < t.rows_valid)) {
+        bf16_t* o = dpre_t + (size_t)((uint32_t)row * 2u) * f;
+        store_nt8(o, pack4(dg[0], dg[1], dg[2], dg[3]));
+        store_nt8(o + f, pack4(du[0], du[1], du[2], du[3]));
+        if (!KEPT) store_nt8(h_t + (size_t)row * f, pack4(h[0], h[1], h[2], h[3]));
+      }
+    }
+  }
+}
+
+template <int EPI, int ACT>
+__device__ __forceinline__ void gated_epilogue(unsigned char* stage, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wave) {
+  const int wm = dma_wave_wm(wave), wn = wave & 1, hh = wave >> 2;
+  unsigned char* patch = stage + wave * 4096;
+  if (EPI == EPI_FWD1) {
+    const int c0 = t.n0 + (dma_wave_cb0(wave) >> 1) * 32;
+    if (t.rows_valid == BM && t.n0 + GN <= p.f) gated_fwd_rounds<ACT, true>((lds_byte_t*)patch, acc, p, t, wm, c0);
+    else gated_fwd_rounds<ACT, false>((lds_byte_t*)patch, acc, p, t, wm, c0);
+  } else {
+    const int col_base = t.n0 + wn * (NB * 32);
+    if (t.rows_valid == BM && t.n0 + BN <= p.f) gated_dh_rounds<ACT, EPI == EPI_DHQ, true>((float*)patch, hh, acc, p, t, wm, col_base);
+    else gated_dh_rounds<ACT, EPI == EPI_DHQ, false>((float*)patch, hh, acc, p, t, wm, col_base);
+  }
+}
+#define FLEXMOE_BY_ACT(act, call)                       \
+  switch (act) {                                        \
+    case FLEXMOE_RELU: { constexpr int ACT = FLEXMOE_RELU; call; break; }          \
+    case FLEXMOE_GELU_ERF: { constexpr int ACT = FLEXMOE_GELU_ERF; call; break; }  \
+    case FLEXMOE_GELU_TANH: { constexpr int ACT = FLEXMOE_GELU_TANH; call; break; } \
+    default: { constexpr int ACT = FLEXMOE_SILU; call; break; }                    \
+  }
+
+// The persistent kernel of either product (see rows_gemm_persist_bf16): 256 workgroups walk the tiles, the next tile's first loads go out
+// while the current K loop drains.  K a multiple of 128.  EPI_FWD1: a tile is 256 rows x 128 columns of H; EPI_DH, EPI_DHQ: 256 of dH.
+template <int EPI> __global__ __launch_bounds__(kDmaThreads) void gated_persist_bf16(const GatedArgs p, const i32x4* row_tab) {
+  constexpr bool FWD = EPI == EPI_FWD1;
+  __shared__ __align__(1024) unsigned char stage0[kDmaStageBytes];
+  __shared__ __align__(1024) unsigned char stage1[kDmaStageBytes];
+  __shared__ __align__(1024) unsigned char stage2[kDmaStageBytes];
+  __shared__ __align__(1024) unsigned char stage3[kDmaStageBytes];
+  lds_byte_t* const s0 = (lds_byte_t*)stage0;
+  lds_byte_t* const s1 = (lds_byte_t*)stage1;
+  lds_byte_t* const s2 = (lds_byte_t*)stage2;
+  lds_byte_t* const s3 = (lds_byte_t*)stage3;
+  typedef typename std::conditional<FWD, DmaSrcGate, DmaSrc>::type WSrc;
+  typedef RowsIssueV<WSrc> Issue;
+
+  const RowTabPtr tab = (RowTabPtr)row_tab;
+  const int K = p.K, f = p.f;
+  const TileSeq seq = make_tile_seq(tab[0][0], p.col_tiles, false, K / DK);
+  const unsigned G = gridDim.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = dma_wave_wm(wave), cb0 = dma_wave_cb0(wave);
+  auto fetch_tile = [&](const TileId& id) {
+    const i32x4 d = tab[1 + id.rt];
+    RowTile t;
+    t.row0 = d[0];
+    t.rows_valid = d[1];
+    t.e = d[2];
+    t.n0 = id.ct * (FWD ? GN : BN);
+    t.cols_valid = min(FWD ? GN : BN, f - t.n0);
+    return t;
+  };
+  auto make_issue = [&](const RowTile& t) {
+    Issue is;
+    is.a_src.init(p.in + (size_t)t.row0 * K, K, t.rows_valid);
+    if constexpr (FWD) is.w_src.init(p.w + (size_t)t.e * K * 2 * f + t.n0, f, t.cols_valid);
+    else is.w_src.init(p.w + (size_t)t.e * K * f + (size_t)t.n0 * K, K, t.cols_valid);
+    is.k_next = 0;
+    return is;
+  };
+  unsigned idx = blockIdx.x;
+  TileId id;
+  if (!find_tile(seq, &idx, G, &id)) return;
+  RowTile t = fetch_tile(id);
+  Issue issue = make_issue(t);
+  dma_prefetch3(s0, s1, s2, issue);
+  for (;;) {
+    DmaAcc acc;
+    zero_acc(acc);
+    unsigned nidx = idx + G;
+    TileId nid;
+    const bool has_next = find_tile(seq, &nidx, G, &nid);
+    const RowTile tn = has_next ? fetch_tile(nid) : t;   // (none: this tile's first loads once more, waited for below and never used)
+    Issue next;
+    dma_pipeline_cont<false, FWD>(s0, s1, s2, s3, acc, issue, K / DK, next, wm, cb0, []() {}, [&](Issue& nx) { nx = make_issue(tn); });
+    FLEXMOE_BY_ACT(p.act, (gated_epilogue<EPI, ACT>(stage3, acc, p, t, wave)))
+    if (!has_next) break;
+    t = tn;
+    issue = next;
+    idx = nidx;
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): nothing may still be landing in LDS when the workgroup ends
+}
+
+// ---- register-staged kernels: any K that is a multiple of 8 -------------------------------------
+// KStridedSrc with the columns of DmaSrcGate.
+struct KStridedGateSrc : KStridedSrc {
+  __device__ __forceinline__ void init(int f, int cols_valid) {
+    const int c = threadIdx.x & 31, kc = threadIdx.x >> 5;
+    const int in_half = min((c >> 3) * 4 + (c & 3), cols_valid / 8 - 1);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      off[j] = (uint32_t)(kc * 8 + j) * 2u * (uint32_t)f + (uint32_t)in_half * 8u + ((c >> 2) & 1 ? (uint32_t)f : 0u);
+  }
+};
+// Lane L of a wave's 32 x 32 accumulator tile [i][j]: row L % 32, columns 8 (q / 4) + 4 (L / 32) + q % 4.  The outputs go out from there,
+// 8 bytes per lane: the products that come here are small or odd.
+template <int EPI, int ACT>
+__device__ __forceinline__ void gated_direct(const f32x16 (&acc)[MB][NB], const GatedArgs& p, const RowTile& t, int wm, int wn) {
+  const int lane = threadIdx.x & 63, f = p.f;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int row = (wm + 2 * i) * 32 + (lane & 31);
+    if (row >= t.rows_valid) continue;
+    const size_t grow = t.row0 + row;
+#pragma unroll
+    for (int j = 0; j < NB; j += EPI == EPI_FWD1 ? 2 : 1)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int in_blk = 8 * g + 4 * (lane >> 5);
+        if (EPI == EPI_FWD1) {
+          const int col = t.n0 + ((wn * NB + j) >> 1) * 32 + in_blk;
+          if (col >= f) continue;
+          float z[4], u[4], h[4], b[4] = {}, bu[4] = {}, da;
+          if (p.bias) {
+            unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + col), b);
+            unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + f + col), bu);
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            z[q] = acc[i][j][4 * g + q] + b[q];
+            u[q] = acc[i][j + 1 < NB ? j + 1 : j][4 * g + q] + bu[q];
+            gate_act<ACT>(z[q], &h[q], &da);
+            h[q] *= u[q];
+          }
+          if (p.out0) {
+            *(uint2*)(p.out0 + grow * 2 * f + col) = pack4(z[0], z[1], z[2], z[3]);
+            *(uint2*)(p.out0 + grow * 2 * f + f + col) = pack4(u[0], u[1], u[2], u[3]);
+          }
+          *(uint2*)(p.out1 + grow * f + col) = pack4(h[0], h[1], h[2], h[3]);
+        } else {
+          const int col = t.n0 + (wn * NB + j) * 32 + in_blk;
+          if (col >= f) continue;
+          float z[4], u[4], dg[4], du[4], h[4];
+          unpack4(*(const uint2*)(p.hpre_in + grow * 2 * f + col), z);
+          unpack4(*(const uint2*)(p.hpre_in + grow * 2 * f + f + col), u);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float dh = acc[i][j][4 * g + q];
+            float a, da;
+            gate_act<ACT>(z[q], &a, &da);
+            dg[q] = dh * u[q] * da;
+            du[q] = dh * a;
+            h[q] = a * u[q];
+          }
+          *(uint2*)(p.out0 + grow * 2 * f + col) = pack4(dg[0], dg[1], dg[2], dg[3]);
+          *(uint2*)(p.out0 + grow * 2 * f + f + col) = pack4(du[0], du[1], du[2], du[3]);
+          if (EPI == EPI_DH) *(uint2*)(p.out1 + grow * f + col) = pack4(h[0], h[1], h[2], h[3]);
+        }
+      }
+  }
+}
+template <int EPI> __global__ __launch_bounds__(kGemmThreads) void gated_staged_bf16(const GatedArgs p) {
+  constexpr bool FWD = EPI == EPI_FWD1;
+  __shared__ __align__(16) unsigned char smem_raw[kGemmLds];
+  bf16_t* smem = (bf16_t*)smem_raw;
+  __shared__ int s_tile[4];
+  RowTile t;
+  if (!lookup_row_tile(p.voff, p.owner, p.V, p.f, p.row_tiles_max, p.col_tiles, blockIdx.x, s_tile, &t)) return;
+  t.n0 = t.n0 / BN * (FWD ? GN : BN);
+  t.cols_valid = min(FWD ? GN : BN, p.f - t.n0);
+  const int K = p.K, f = p.f, KT = (K + BK - 1) / BK;
+  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  f32x16 acc[MB][NB];
+  zero_acc(acc);
+  KContigSrc a_src;
+  a_src.init(p.in + (size_t)t.row0 * K, K, t.rows_valid, K);
+  int ka = 0, kb = 0;
+  auto load_a = [&](uint4 (&ra)[8]) {
+    a_src.load(ra, ka);
+    ka += BK;
+  };
+  if constexpr (FWD) {
+    KStridedGateSrc w_src;
+    w_src.init(f, t.cols_valid);
+    const bf16_t* wp = p.w + (size_t)t.e * K * 2 * f + t.n0;
+    auto load_b = [&](uint4 (&rb)[8]) {
+      w_src.load(rb, wp + (size_t)kb * 2 * f, K - kb);
+      kb += BK;
+    };
+    run_pipeline<true>(smem, acc, KT, KContigSrc::store, KStridedSrc::store, load_a, load_b, wm, wn, 8);
+  } else {
+    KContigSrc w_src;
+    w_src.init(p.w + (size_t)t.e * K * f + (size_t)t.n0 * K, K, t.cols_valid, K);
+    auto load_b = [&](uint4 (&rb)[8]) {
+      w_src.load(rb, kb);
+      kb += BK;
+    };
+    run_pipeline<true>(smem, acc, KT, KContigSrc::store, KContigSrc::store, load_a, load_b, wm, wn, 8);
+  }
+  FLEXMOE_BY_ACT(p.act, (gated_direct<EPI, ACT>(acc, p, t, wm, wn)))
+}
+
+// ---- few rows ----------------------------------------------------------------------------------
+template <int BM, int EPI> struct GatedSmallPol {
+  const GatedArgs& p;
+  template <int ACT, int RB>
+  __device__ __forceinline__ void out(const f32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg) const {
+    const int f = p.f;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      if (i * 16 + fr >= t.rows) continue;
+      const size_t row = orow[i];
+      if (EPI == EPI_FWD1) {
+        const int col = n0 + wave * 16 + fg * 4;
+        if (col >= f) continue;
+        f32x4 g = acc[i][0], u = acc[i][1];
+        if (p.bias) {
+          float b[4], bu[4];
+          unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + col), b);
+          unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + f + col), bu);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            g[q] += b[q];
+            u[q] += bu[q];
+          }
+        }
+        float h[4], da;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          gate_act<ACT>(g[q], &h[q], &da);
+          h[q] *= u[q];
+        }
+        if (p.out0) {
+          *(uint2*)(p.out0 + row * 2 * f + col) = pack4(g[0], g[1], g[2], g[3]);
+          *(uint2*)(p.out0 + row * 2 * f + f + col) = pack4(u[0], u[1], u[2], u[3]);
+        }
+        *(uint2*)(p.out1 + row * f + col) = pack4(h[0], h[1], h[2], h[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int col = n0 + wave * 32 + j * 16 + fg * 4;
+          if (col >= f) continue;
+          float g[4], u[4], dg[4], du[4], h[4];
+          unpack4(*(const uint2*)(p.hpre_in + row * 2 * f + col), g);
+          unpack4(*(const uint2*)(p.hpre_in + row * 2 * f + f + col), u);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float dh = acc[i][j][q];
+            float a, da;
+            gate_act<ACT>(g[q], &a, &da);
+            dg[q] = dh * u[q] * da;
+            du[q] = dh * a;
+            h[q] = a * u[q];
+          }
+          *(uint2*)(p.out0 + row * 2 * f + col) = pack4(dg[0], dg[1], dg[2], dg[3]);
+          *(uint2*)(p.out0 + row * 2 * f + f + col) = pack4(du[0], du[1], du[2], du[3]);
+          if (EPI == EPI_DH) *(uint2*)(p.out1 + row * f + col) = pack4(h[0], h[1], h[2], h[3]);
+        }
+      }
+    }
+  }
+  template <int RB>
+  __device__ __forceinline__ void epilogue(const f32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg) const {
+    FLEXMOE_BY_ACT(p.act, (out<ACT, RB>(acc, t, orow, n0, wave, fr, fg)))
+  }
+};
+template <int BM, int EPI> __global__ __launch_bounds__(kSmallThreads, 2) void gated_small_bf16(const SmallCore c, const GatedArgs p) {
+  __shared__ __align__(1024) unsigned char smem[SmallCfg<BM>::kLds];
+  const GatedSmallPol<BM, EPI> pol{p};
+  small_core<BM, EPI != EPI_FWD1, EPI == EPI_FWD1, f32x4>(c, pol, smem, blockIdx.x, gridDim.x);
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+// a: planned as a layer with a.f = 2 f (rows_kernels)
+template <int EPI>
+static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, const void* bias, const void* hpre_in, void* out0, void* out1,
+                               void* ws, hipStream_t s) {
+  constexpr bool FWD = EPI == EPI_FWD1;
+  const int f = a.f / 2, K = a.d;
+  const RowsKernels rk = rows_kernels(a, ws);
+  GatedArgs p{(const bf16_t*)in, (const bf16_t*)w, (const bf16_t*)bias, a.voff, a.owner, a.V, K, f, a.A / BM + a.V, 0,
+              (const bf16_t*)hpre_in, (bf16_t*)out0, (bf16_t*)out1, a.act};
+  if (rk.small.bm) {
+    const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, K, FWD ? 2 * f : f, FWD ? (f + SN / 2 - 1) / (SN / 2) : (f + SN - 1) / SN,
+                      nullptr, 1, rk.small_partial, rk.small.counters};
+    const long long most = ((long long)a.A / rk.small.bm + a.E) * c.col_tiles * kSmallSplitMax;
+    const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
+    if (rk.small.bm == 32) hipLaunchKernelGGL((gated_small_bf16<32, EPI>), grid, dim3(kSmallThreads), 0, s, c, p);
+    else hipLaunchKernelGGL((gated_small_bf16<64, EPI>), grid, dim3(kSmallThreads), 0, s, c, p);
+    return hipGetLastError();
+  }
+  p.col_tiles = FWD ? (f + GN - 1) / GN : (f + BN - 1) / BN;
+  const unsigned grid = patched_grid(p.row_tiles_max, p.col_tiles);
+  if (K % 128 == 0)
+    hipLaunchKernelGGL((gated_persist_bf16<EPI>), dim3(std::min(grid, 256u)), dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
+  else
+    hipLaunchKernelGGL((gated_staged_bf16<EPI>), dim3(grid), dim3(kGemmThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+static FfnArgs doubled(const FfnArgs& a) {
+  FfnArgs b = a;
+  b.f = 2 * a.f;
+  return b;
+}
+
+hipError_t launch_ffn_gated_fwd_bf16(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
+                                     void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s) {
+  if (a.A == 0) return hipSuccess;
+  const FfnArgs a2 = doubled(a);
+  launch_rows_plan(a2, ws, s);
+  void* h = h_keep ? h_keep : ws;
+  const hipError_t err = launch_gated<EPI_FWD1>(a2, xp, w1, b1, nullptr, hpre, h, ws, s);
+  if (err != hipSuccess) return err;
+  return launch_rows_plain(a2, h, w2, b2, a.f, yp, ws, s);
+}
+
+hipError_t launch_ffn_gated_bwd_bf16(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept, const void* w1,
+                                     const void* w2, void* dxp, void* dw1, void* dw2, void* ws, hipStream_t s) {
+  const FfnArgs a2 = doubled(a);
+  bf16_t* dhpre = (bf16_t*)ws;
+  bf16_t* h_ws = (bf16_t*)((char*)ws + align_up((size_t)a2.A * a2.f * sizeof(bf16_t), 256));
+  launch_bwd_plan(a2, a.f, ws, s);
+  if (a.A > 0) {
+    const hipError_t err = h_kept ? launch_gated<EPI_DHQ>(a2, dyp, w2, nullptr, hpre, dhpre, nullptr, ws, s)
+                                  : launch_gated<EPI_DH>(a2, dyp, w2, nullptr, hpre, dhpre, h_ws, ws, s);
+    if (err != hipSuccess) return err;
+  }
+  return launch_bwd_products(a2, a.f, h_kept ? h_kept : h_ws, dyp, dw2, xp, dhpre, dw1, w1, dxp, nullptr, ws, s);
+}
+
+}  // namespace flexmoe

@@ -1,0 +1,232 @@
+// The few-rows rows product of ffn_bf16_small.h with its element type, weight columns and epilogue left open: gated experts
+// (ffn_gated.hip) and 8-bit integer experts (ffn_i8.hip).
+#pragma once
+#include "common.h"
+#include "ffn_bf16_tile.h"
+#include "ffn_bf16_dma.h"
+#include "ffn_bf16_persist.h"
+#include "ffn_bf16_small.h"
+namespace flexmoe {
+// =============================================================================================
+// Tiles, row list, stages, segments and their sum are those of rows_gemm_small_bf16 (see there for why), on the same plan.  What is
+// open:
+//  * V4, the type of four sums: f32x4 (bf16 operands) or i32x4 (8-bit integers, 128 of them to a stage: one instruction takes the
+//    same 16 bytes per lane in either case).  K and the operands' offsets count two-byte units, so 8-bit operands pass K / 2.
+//    Sums of integers are exact: segments change nothing, and a row's bits do not depend on the other rows.
+//  * GATED: the tile's 128 weight columns are 64 columns of the first half (gate) and the same 64 of the second (up), 16 and 16 in
+//    turn, so that a wave holds both values of an output in the same lane: acc[i][0] and acc[i][1].
+//  * rows of `in` are addressed with 64 bits, so any number of rows is served.
+//  * pol.epilogue(acc, tile, ...) does the rest.
+// =============================================================================================
+struct SmallCore {
+  const bf16_t* in;              // [rows, K]
+  const bf16_t* w;               // WT: [E, NC, K], else [E, K, NC]
+  const i32x4* tab;              // as SmallArgs
+  const int32_t* rowmap;
+  int K, NC, col_tiles;          // NC: all weight columns (GATED: both halves)
+  const int32_t* gsrc;           // gathered rows of `in`: row gsrc[bucket row] / gk; or null
+  int gk;
+  float* partial;
+  int* counters;
+};
+struct SmallTile {
+  int first, rows, e, ct;        // position in rowmap, rows, expert, column tile
+};
+
+template <int BM, bool WT, bool GATED, typename V4, typename Pol>
+__device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, unsigned char* smem, unsigned block, unsigned blocks) {
+  typedef SmallCfg<BM> C;
+  constexpr int S = C::S, RB = BM / 16, NB2 = SN / kSmallWaves / 16;      // 16-row and 16-column blocks of a wave
+  lds_byte_t* const sm = (lds_byte_t*)smem;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)sm);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int fr = lane & 15, fg = lane >> 4;              // fragment row (or column), group of 16 bytes of k
+  const RowTabPtr tab = (RowTabPtr)p.tab;
+  const int K = p.K, NC = p.NC, half = NC / 2;
+  const int rows_act = tab[0][0];
+  const int k_tiles = (K + SK - 1) / SK;
+  const int tiles = rows_act * p.col_tiles;
+  const int nseg = small_segments(tiles, k_tiles);
+  // without segments: the XCD-aware patch order; with them: tile-major, a tile's segments side by side
+  const unsigned total = nseg > 1 ? (unsigned)(tiles * nseg) : patched_grid(rows_act, p.col_tiles);
+
+  uint32_t la, lw;                                       // lane parts of the LDS fragment addresses
+  la = fr * 128 + ((fg ^ (fr & 7)) << 4);                // second half of a stage: chunk index XOR 4
+  if (WT) {
+    lw = C::kABytes + wave * (NB2 * 2048) + la;
+  } else {
+    const int k = 8 * fg + (fr >> 2);
+    const int x = ((fr >> 2) << 2) ^ ((fg & 1) << 1);
+    lw = C::kABytes + k * 256 + (((wave * (NB2 * 2) + ((fr & 3) >> 1)) ^ x) << 4) + 8 * (fr & 1);
+  }
+
+  for (unsigned idx = block; idx < total; idx += blocks) {
+    int rt, ct, seg = 0;
+    if (nseg > 1) {
+      seg = (int)(idx % nseg);
+      const int tile = (int)(idx / nseg);
+      rt = tile / p.col_tiles;
+      ct = tile % p.col_tiles;
+    } else if (!patched_tile(idx, rows_act, p.col_tiles, &rt, &ct)) {
+      continue;
+    }
+    const i32x4 d = tab[1 + rt];
+    const SmallTile t{d[0], d[1], d[2], ct};
+    // first column of the tile, and columns there are (GATED: of either half)
+    const int n0 = ct * (GATED ? SN / 2 : SN), cols = min(GATED ? SN / 2 : SN, (GATED ? half : NC) - n0);
+    const int kt0 = (int)((long long)k_tiles * seg / nseg), kt1 = (int)((long long)k_tiles * (seg + 1) / nseg);
+    const bf16_t* w_e = p.w + (size_t)t.e * K * NC + (WT ? (size_t)n0 * K : (size_t)n0);
+
+    // rows of the wave's loads (rows past the tile repeat its last row) and of its outputs
+    const bf16_t* aptr[C::kALoads];
+    int akc;                                             // the lane's chunk of a row, in two-byte units
+    {
+      const int lr = lane >> 3;
+      akc = ((lane & 7) ^ lr) * 8;
+#pragma unroll
+      for (int q = 0; q < C::kALoads; ++q) {
+        int r = p.rowmap[t.first + min((wave * C::kALoads + q) * 8 + lr, t.rows - 1)];
+        if (p.gsrc) r = p.gsrc[r] / p.gk;
+        aptr[q] = p.in + (size_t)r * K + akc;
+      }
+    }
+    int orow[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) orow[b] = p.rowmap[t.first + min(b * 16 + fr, t.rows - 1)];
+    uint32_t woff[C::kWLoads];
+    int wk[C::kWLoads];                                  // k (in the stage) of the lane's first element
+    size_t wbase[C::kWLoads];                            // (uniform) where the load's rows start behind w_e: GATED && WT, the up half
+#pragma unroll
+    for (int q = 0; q < C::kWLoads; ++q) {
+      const int i = wave * C::kWLoads + q;
+      wbase[q] = 0;
+      if (WT) {
+        int row = i * 8 + (lane >> 3);
+        wk[q] = ((lane & 7) ^ (row & 7)) * 8;
+        if (GATED) {
+          row = (row >> 5) * 16 + (row & 15);
+          if ((i >> 1) & 1) wbase[q] = (size_t)half * K;
+        }
+        woff[q] = (uint32_t)((uint32_t)min(row, cols - 1) * (uint32_t)K + wk[q]) * 2;
+      } else {
+        const int kr = i * 4 + (lane >> 4);
+        wk[q] = kr;
+        int c = (lane & 15) ^ ((kr & 3) << 2) ^ ((kr & 8) >> 2), up = 0;
+        if (GATED) {
+          up = (c >> 1) & 1 ? half : 0;
+          c = (c >> 2) * 2 + (c & 1);
+        }
+        woff[q] = (uint32_t)(kr * NC + min(c, cols / 8 - 1) * 8 + up) * 2;
+      }
+    }
+    auto issue = [&](int kt) {
+      const unsigned st = lds0 + (unsigned)((kt - kt0) % S) * C::kStage;
+      const int k0 = kt * SK;
+      const bf16_t* wb = w_e + (WT ? (size_t)k0 : (size_t)k0 * NC);
+      if (k0 + SK <= K) {
+#pragma unroll
+        for (int q = 0; q < C::kALoads; ++q) small_load_at(aptr[q] + k0, st + (wave * C::kALoads + q) * 1024);
+#pragma unroll
+        for (int q = 0; q < C::kWLoads; ++q) small_load(wb + wbase[q], woff[q], st + C::kABytes + (wave * C::kWLoads + q) * 1024);
+      } else {                                           // past K: zeros on both sides
+        const bf16_t* z = (const bf16_t*)kSmallZero + (lane & 7) * 8;
+#pragma unroll
+        for (int q = 0; q < C::kALoads; ++q) small_load_at(k0 + akc < K ? aptr[q] + k0 : z, st + (wave * C::kALoads + q) * 1024);
+#pragma unroll
+        for (int q = 0; q < C::kWLoads; ++q)
+          small_load_at(k0 + wk[q] < K ? (const bf16_t*)((const char*)(wb + wbase[q]) + woff[q]) : z,
+                        st + C::kABytes + (wave * C::kWLoads + q) * 1024);
+      }
+    };
+
+    V4 acc[RB][NB2];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB2; ++j) acc[i][j] = V4{0, 0, 0, 0};
+
+    __syncthreads();                                     // the previous tile's epilogue has left the stages
+#pragma unroll
+    for (int q = 0; q < S - 1; ++q)
+      if (kt0 + q < kt1) issue(kt0 + q);
+    for (int kt = kt0; kt < kt1; ++kt) {
+      small_wait<C::kLoads>(min(S - 2, kt1 - 1 - kt));
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      if (kt + S - 1 < kt1) issue(kt + S - 1);           // into the stage every wave has just left
+      const lds_byte_t* st = sm + ((kt - kt0) % S) * C::kStage;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8 a[RB], w[NB2];
+#pragma unroll
+        for (int j = 0; j < NB2; ++j) {
+          if (WT) {
+            w[j] = *(const __attribute__((address_space(3))) bf16x8*)(st + (lw ^ (ks << 6)) + j * 2048);
+          } else {
+            const lds_byte_t* at = st + (lw ^ (uint32_t)(j << 5)) + ks * (32 * 256);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 4 * 256));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            w[j] = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < RB; ++i) a[i] = *(const __attribute__((address_space(3))) bf16x8*)(st + (la ^ (ks << 6)) + i * 2048);
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB2; ++j) acc[i][j] = mma_16x16(w[j], a[i], acc[i][j]);
+      }
+    }
+    __syncthreads();                                     // every wave has left the last stage
+
+    if (nseg > 1) {
+      // partial tiles cross XCDs: see rows_gemm_small_bf16
+      const int tile = rt * p.col_tiles + ct;
+      typedef unsigned long long u64;
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      u64* part = (u64*)(p.partial + (size_t)tile * nseg * (BM * SN));
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB2; ++j) {
+          u64* dst = part + (size_t)seg * (BM * SN / 2) + (i * NB2 + j) * (2 * kSmallThreads) + threadIdx.x;
+          const u32x4 bits = __builtin_bit_cast(u32x4, acc[i][j]);
+          __hip_atomic_store(dst, (u64)bits[0] | (u64)bits[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          __hip_atomic_store(dst + kSmallThreads, (u64)bits[2] | (u64)bits[3] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the stores have arrived
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const int before = __hip_atomic_fetch_add(&p.counters[tile], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == nseg - 1) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        *(volatile __attribute__((address_space(3))) int*)sm = before;
+      }
+      __syncthreads();
+      const bool last = __builtin_amdgcn_readfirstlane(*(volatile __attribute__((address_space(3))) int*)sm) == nseg - 1;
+      if (!last) continue;
+      if (threadIdx.x == 0) p.counters[tile] = 0;        // as the plan left it: the call's next product counts there too
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB2; ++j) {
+          V4 s = V4{0, 0, 0, 0};
+          for (int g = 0; g < nseg; ++g) {
+            u64* from = part + (size_t)g * (BM * SN / 2) + (i * NB2 + j) * (2 * kSmallThreads) + threadIdx.x;
+            const u64 lo = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const u64 hi = __hip_atomic_load(from + kSmallThreads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s += __builtin_bit_cast(V4, u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)});
+          }
+          acc[i][j] = s;
+        }
+      __syncthreads();                                   // the flag has been read
+    }
+    // lane: row 16 i + fr of the tile (bucket row orow[i], there if 16 i + fr < rows), four columns from 4 fg on of 16-column block
+    // 2 wave + j (GATED: j = 0 gate, 1 up, of columns n0 + 16 wave + 4 fg ..)
+    pol.epilogue(acc, t, orow, n0, wave, fr, fg);
+  }
+}
+
+}  // namespace flexmoe

@@ -1,0 +1,377 @@
+"""Gated expert FFN (flexmoe_expert_ffn_gated_fwd / _bwd) against the formulas in 64 bits.
+
+Tolerances.  u = finfo(t).eps / 2 is the relative error of one rounding.  An output is a sum of products, rounded at the end; what its
+factors are off by goes into it as independent errors: a sum of terms that are each off by at most n_i is off by 6 / sqrt(3) sqrt(sum n_i^2)
+(six standard deviations of errors uniform in +-n_i).  Errors of the factors (`noise` below):
+  * a rounding to dtype (H, dHpre): u of the value;
+  * a sum of K fp32 products (G, U, dH, and every output): 2^-23 sqrt(K) of the root of the sum of its squared terms;
+  * act(z) and act'(z): 2^-20 (|z| + 1), absolute -- both are sums of parts of up to |z| + 1 that may cancel, each from fp32 functions or (bf16)
+    the hardware's exponential and reciprocal (2^-23 each, |z| times that through the exponent) and an error function within 2^-22.6.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+ACTS = ("relu", "gelu_erf", "gelu_tanh", "silu")
+
+
+def _b():
+    from paper_2304_03946_amd import binding as B
+    B.load_library()
+    return B
+
+
+def act64(kind, z):
+    if kind == "relu":
+        return z.clamp(min=0), (z > 0).to(z.dtype)
+    if kind == "silu":
+        s = torch.sigmoid(z)
+        return z * s, s * (1 + z * (1 - s))
+    if kind == "gelu_erf":
+        cdf = 0.5 * torch.erfc(-z / math.sqrt(2))
+        return z * cdf, cdf + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    c = math.sqrt(2 / math.pi)
+    t = torch.tanh(c * (z + 0.044715 * z ** 3))
+    return 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z)
+
+
+SPREAD = 6 / math.sqrt(3)
+
+
+def sums(K):
+    return 2.0 ** -23 * math.sqrt(K)
+
+
+def dot(p, q):
+    return torch.sqrt((p * p) @ (q * q).contiguous())
+
+
+def forward64(x, w1, b1, w2, b2, rows, act, u=0.0):
+    """rows: expert of every row.  -> {output: (value, noise)}."""
+    A, f, d = x.shape[0], w2.shape[1], w2.shape[2]
+    out = {n: (x.new_zeros(A, c), x.new_zeros(A, c)) for n, c in (("hpre", 2 * f), ("h", f), ("y", d))}
+    for e in range(w1.shape[0]):
+        r = torch.nonzero(rows == e).flatten()
+        if len(r) == 0:
+            continue
+        z = x[r] @ w1[e] + (b1[e] if b1 is not None else 0)
+        nz = SPREAD * sums(d) * dot(x[r], w1[e]) + 2.0 ** -23 * z.abs()
+        g, up = z[:, :f], z[:, f:]
+        a = act64(act, g)[0]
+        h = a * up
+        nh = 1.13 * nz[:, :f] * up.abs() + nz[:, f:] * a.abs() + 2.0 ** -20 * (g.abs() + 1) * up.abs()      # (|act'| < 1.13)
+        y = h @ w2[e] + (b2[e] if b2 is not None else 0)
+        ny = SPREAD * (dot(nh + u * h.abs(), w2[e]) + sums(f) * dot(h, w2[e])) + 2.0 ** -23 * y.abs()
+        for n, v, noise in (("hpre", z, nz), ("h", h, nh), ("y", y, ny)):
+            out[n][0][r], out[n][1][r] = v, noise
+    return out
+
+
+def backward64(dy, x, hpre, h, w1, w2, rows, act, u=0.0):
+    """-> {output: (value, noise)} and dz, the unrounded dHpre."""
+    A, f, E = x.shape[0], w2.shape[1], w1.shape[0]
+    g, up = hpre[:, :f], hpre[:, f:]
+    a, da = act64(act, g)
+    na = 2.0 ** -20 * (g.abs() + 1)
+    hh, nh = (a * up, na * up.abs() + u * (a * up).abs()) if h is None else (h, torch.zeros_like(h))
+    dz, ndz = x.new_zeros(A, 2 * f), x.new_zeros(A, 2 * f)
+    out = {n: (torch.zeros_like(t), torch.zeros_like(t)) for n, t in (("dxp", x), ("dw1", w1), ("dw2", w2))}
+    for e in range(E):
+        r = torch.nonzero(rows == e).flatten()
+        if len(r) == 0:
+            continue
+        w2t = w2[e].T.contiguous()
+        dh, ndh = dy[r] @ w2t, SPREAD * sums(w2.shape[2]) * dot(dy[r], w2t)
+        z = torch.cat([dh * up[r] * da[r], dh * a[r]], 1)
+        nz = torch.cat([up[r].abs() * (ndh * da[r].abs() + dh.abs() * na[r]), ndh * a[r].abs() + dh.abs() * na[r]], 1) + (u + 2.0 ** -22) * z.abs()
+        dz[r], ndz[r] = z, nz
+        w1t, xt, ht = w1[e].T.contiguous(), x[r].T.contiguous(), hh[r].T.contiguous()
+        n = len(r)
+        for name, at, v, noise in (
+                ("dxp", r, z @ w1t, dot(nz, w1t) + sums(2 * f) * dot(z, w1t)),
+                ("dw1", e, xt @ z, dot(xt, nz) + sums(n) * dot(xt, z)),
+                ("dw2", e, ht @ dy[r], dot(nh[r].T.contiguous(), dy[r]) + sums(n) * dot(ht, dy[r]))):
+            out[name][0][at], out[name][1][at] = v, SPREAD * noise
+    return out, dz, ndz
+
+
+def buckets(counts, E, seed=0):
+    """counts: rows per vExpert; owners: every expert once, then the rest at random, shuffled."""
+    rng = np.random.default_rng(seed)
+    V = len(counts)
+    owner = np.concatenate([np.arange(E), rng.integers(0, E, V - E)]).astype(np.int32)
+    rng.shuffle(owner)
+    off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    return off, owner, np.repeat(owner, counts)
+
+
+def split(total, V, rng, empty=0.2):
+    w = rng.dirichlet(np.full(V, 0.7)) * (rng.random(V) > empty)
+    w = w / w.sum() if w.sum() > 0 else np.full(V, 1.0 / V)
+    c = np.floor(w * total).astype(int)
+    c[int(np.argmax(c))] += total - c.sum()
+    return c
+
+
+class Case:
+    def __init__(self, A, d, f, E, V, dtype, act, bias, seed=0, counts=None):
+        B = _b()
+        rng = np.random.default_rng(seed)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed)
+        self.A, self.d, self.f, self.E, self.V, self.act = A, d, f, E, V, act
+        self.dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        off, owner, rows = buckets(split(A, V, rng) if counts is None else counts, E, seed)
+        self.voff, self.owner = torch.from_numpy(off).cuda(), torch.from_numpy(owner).cuda()
+        self.rows = torch.from_numpy(rows).cuda()
+
+        def new(*s, std=1.0):
+            return (torch.randn(*s, generator=gen, device="cuda") * std).to(self.dt)
+        self.x, self.dy = new(A, d), new(A, d)
+        self.w1, self.w2 = new(E, d, 2 * f, std=1 / math.sqrt(d)), new(E, f, d, std=1 / math.sqrt(f))
+        self.b1, self.b2 = (new(E, 2 * f, std=0.3), new(E, d, std=0.3)) if bias else (None, None)
+        code = B.BF16 if dtype == "bf16" else B.F32
+        self.code = dict(relu=B.RELU, gelu_erf=B.GELU_ERF, gelu_tanh=B.GELU_TANH, silu=B.SILU)[act]
+        self.ws = torch.empty(B.flexmoe_workspace_bytes(max(A, 1), d, 2 * f, E, 1, V, code), dtype=torch.uint8, device="cuda")
+        self.hpre, self.h, self.y = new(A, 2 * f), new(A, f), new(A, d)
+        self.dxp, self.dw1, self.dw2 = new(A, d), torch.full_like(self.w1, 7), torch.full_like(self.w2, 7)
+
+    def fwd(self, keep=True, keep_h=True):
+        _b().flexmoe_expert_ffn_gated_fwd(self.x, self.voff, self.owner, self.w1, self.b1, self.w2, self.b2, self.code,
+                                          self.hpre if keep else None, self.y, self.ws, h=self.h if keep_h else None)
+
+    def bwd(self, kept=True):
+        _b().flexmoe_expert_ffn_gated_bwd(self.dy, self.x, self.hpre, self.w1, self.w2, self.voff, self.owner, self.code, self.dxp,
+                                          self.dw1, self.dw2, self.ws, h=self.h if kept else None)
+
+    def close(self, name, got, want, noise):
+        u = torch.finfo(self.dt).eps / 2
+        err, tol = (got.double() - want).abs(), u * want.abs() + (1 + u) * noise + 1e-37
+        worst = float((err / tol).max()) if err.numel() else 0.0
+        assert worst <= 1 + 2 * u, f"{name}: {worst:.3f} of the tolerance"
+
+    def u(self):
+        return torch.finfo(self.dt).eps / 2
+
+    def check_fwd(self):
+        b1, b2 = (None, None) if self.b1 is None else (self.b1.double(), self.b2.double())
+        out = forward64(self.x.double(), self.w1.double(), b1, self.w2.double(), b2, self.rows, self.act, self.u())
+        for name, got in (("hpre", self.hpre), ("h", self.h), ("y", self.y)):
+            self.close(name, got, *out[name])
+
+    def backward64(self, kept):
+        return backward64(self.dy.double(), self.x.double(), self.hpre.double(), self.h.double() if kept else None, self.w1.double(),
+                          self.w2.double(), self.rows, self.act, self.u())
+
+    def check_bwd(self, kept):
+        out, dz, ndz = self.backward64(kept)
+        for name in ("dxp", "dw1", "dw2"):
+            self.close(name, getattr(self, name), *out[name])
+        return dz, ndz
+
+
+# (rows, d, f, E, V): few rows with 32- and 64-row tiles, with segments and without; 256 x 256 tiles where d is a multiple of 128
+# (direct loads) and where it is not; f in no whole tiles; one row, one expert, empty experts
+FEW = [(1, 8, 8, 1, 1), (3, 64, 72, 4, 5), (17, 1024, 512, 8, 12), (130, 328, 904, 12, 15), (700, 256, 264, 4, 9), (2000, 136, 1032, 3, 3)]
+# (the last but one is just inside the line of the few-rows kernels: (64 + 3 * 200 / 8) * 256 * 256 / 256 = 35584 rows)
+LARGE = [(7300, 2048, 1024, 4, 6), (7300, 2048, 1096, 4, 4), (7400, 2056, 1032, 3, 5), (30000, 128, 200, 2, 40), (31000, 200, 128, 5, 5),
+         (36000, 200, 128, 5, 5)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act,bias", [("silu", True), ("gelu_erf", False), ("gelu_tanh", True), ("relu", False)])
+@pytest.mark.parametrize("A,d,f,E,V", FEW)
+def test_few_rows(A, d, f, E, V, act, bias, dtype):
+    c = Case(A, d, f, E, V, dtype, act, bias, seed=A + d)
+    c.fwd()
+    c.check_fwd()
+    y = c.y.clone()
+    c.fwd(keep=False, keep_h=False)
+    assert torch.equal(y, c.y), "the same output without Hpre and H"
+    for kept in (True, False):
+        c.bwd(kept)
+        c.check_bwd(kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,bias", [("silu", False), ("silu", True), ("gelu_erf", True), ("gelu_tanh", False), ("relu", True)])
+@pytest.mark.parametrize("A,d,f,E,V", LARGE)
+def test_many_rows(A, d, f, E, V, act, bias):
+    from tests.test_dispatch import paths
+    assert paths(A, d, 2 * f, E, V)["few_rows"] == (64 if A == 31000 else 0)
+    c = Case(A, d, f, E, V, "bf16", act, bias, seed=A + d)
+    c.fwd()
+    c.check_fwd()
+    y = c.y.clone()
+    c.fwd(keep=False, keep_h=False)
+    assert torch.equal(y, c.y)
+    for kept in (True, False):
+        c.bwd(kept)
+        c.check_bwd(kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("A,d,f,E,V", [(5000, 192, 320, 4, 6), (4096, 512, 256, 1, 1)])
+def test_many_rows_fp32(A, d, f, E, V):
+    c = Case(A, d, f, E, V, "f32", "silu", True, seed=A)
+    c.fwd()
+    c.check_fwd()
+    for kept in (True, False):
+        c.bwd(kept)
+        c.check_bwd(kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("A,d,f", [(90, 64, 72), (7300, 2048, 1024)])
+def test_bias_gradients(A, d, f, dtype):
+    """flexmoe_expert_bias_grads with 2 f in the place of f reads dHpre where the backward call left it."""
+    if dtype == "f32" and A > 1000:
+        A, d, f = 1500, 128, 96
+    c = Case(A, d, f, 3, 5, dtype, "silu", True, seed=5)
+    c.fwd()
+    c.bwd()
+    db1, db2 = torch.empty_like(c.b1), torch.empty_like(c.b2)
+    _b().flexmoe_expert_bias_grads(c.dy, c.voff, c.owner, 2 * f, 3, db1, db2, c.ws)
+    dz_all, ndz = c.check_bwd(True)
+
+    def norm(t):
+        return torch.sqrt((t * t).sum(0))
+    for e in range(3):
+        sel = c.rows == e
+        dz, dy = dz_all[sel], c.dy.double()[sel]
+        c.close("db1", db1[e], dz.sum(0), SPREAD * (norm(ndz[sel]) + sums(A) * norm(dz)))
+        c.close("db2", db2[e], dy.sum(0), SPREAD * sums(A) * norm(dy))
+
+
+@pytest.mark.gpu
+def test_gradients_are_differences():
+    """fp32 gradients of <y, dy> against central differences of the 64-bit formula and of the kernel's own forward pass' formula."""
+    c = Case(24, 16, 24, 2, 3, "f32", "silu", False, seed=9)
+    c.fwd()
+    c.bwd()
+    x, w1, w2, dy = c.x.double(), c.w1.double(), c.w2.double(), c.dy.double()
+
+    def loss(x_, w1_, w2_):
+        return float((forward64(x_, w1_, None, w2_, None, c.rows, "silu")["y"][0] * dy).sum())
+    rng = np.random.default_rng(1)
+    for name, t, g in (("x", x, c.dxp), ("w1", w1, c.dw1), ("w2", w2, c.dw2)):
+        for _ in range(6):
+            at = tuple(int(rng.integers(0, n)) for n in t.shape)
+            step, keep = 1e-4, t[at].item()
+            t[at] = keep + step
+            up = loss(x, w1, w2)
+            t[at] = keep - step
+            down = loss(x, w1, w2)
+            t[at] = keep
+            # differences: step^2 of a third derivative of order |g| + 1; fp32 sums of 24 rows x 48 terms
+            assert abs((up - down) / (2 * step) - g[at].item()) <= 1e-5 * (1 + abs(g[at].item())), (name, at)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_rows_and_rows_behind_the_last_bucket(dtype):
+    c = Case(0, 64, 72, 4, 5, dtype, "silu", True, counts=[0, 0, 0, 0, 0])
+    c.fwd()
+    c.bwd()
+    assert not c.dw1.any() and not c.dw2.any()
+    for A, d, f in ((40, 64, 72), (7300, 2048, 1024)) if dtype == "bf16" else ((40, 64, 72),):
+        c = Case(A, d, f, 2, 3, dtype, "silu", False, counts=[A // 2 - 9, 0, A // 2])
+        used = int(c.voff[-1])
+        assert used < A
+        c.rows = torch.cat([c.rows, torch.full((A - used,), -1, device="cuda")])
+        old = [t[used:].clone() for t in (c.y, c.hpre, c.h, c.dxp)]
+        c.fwd()
+        c.bwd()
+        for t, o in zip((c.y, c.hpre, c.h, c.dxp), old):
+            assert torch.equal(t[used:], o)
+        out = c.backward64(True)[0]
+        c.close("dw1", c.dw1, *out["dw1"])
+        c.close("dw2", c.dw2, *out["dw2"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("A,d,f,E,V", [(40, 64, 72, 4, 5), (7300, 2048, 1024, 4, 6), (7400, 2056, 1032, 3, 5)])
+def test_non_finite_rows_stay_where_they_are(A, d, f, E, V, dtype):
+    """A NaN and an infinity in one row of x reach that row's outputs and no other's."""
+    if dtype == "f32" and A > 1000:
+        pytest.skip("one set of fp32 kernels: covered by the small case")
+    c = Case(A, d, f, E, V, dtype, "silu", False, seed=3)
+    c.fwd()
+    y = c.y.clone()
+    c.x[A // 2, 3] = float("nan")
+    c.x[A // 3, 0] = float("inf")
+    c.fwd()
+    other = torch.ones(A, dtype=torch.bool, device="cuda")
+    other[[A // 2, A // 3]] = False
+    assert torch.equal(c.y[other], y[other]) and torch.isnan(c.y[A // 2]).all() and not torch.isfinite(c.y[A // 3]).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("A,d,f,E,V", [(16, 1024, 512, 8, 12), (7300, 2048, 1024, 4, 6)])
+def test_equal_calls_streams_and_graphs(A, d, f, E, V):
+    """The same bits again, on another stream and from a graph that is replayed between eager calls with other rows."""
+    c = Case(A, d, f, E, V, "bf16", "silu", True, seed=11)
+
+    def step():
+        c.fwd()
+        c.bwd()
+        return [t.clone() for t in (c.y, c.hpre, c.h, c.dxp, c.dw1, c.dw2)]
+    want = step()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = step()
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.fwd()
+        c.bwd()
+    x0, off0 = c.x.clone(), c.voff.clone()
+    for i in range(3):
+        c.x.copy_(x0 * (i + 2))
+        c.voff[1:-1] = torch.sort(torch.randint(0, A + 1, (V - 1,), device="cuda", dtype=torch.int32)).values
+        eager = step()
+        for t in (c.y, c.hpre, c.h, c.dxp, c.dw1, c.dw2):
+            t.fill_(3)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (c.y, c.hpre, c.h, c.dxp, c.dw1, c.dw2))), i
+        c.x.copy_(x0)
+        c.voff.copy_(off0)
+        assert all(torch.equal(a, b) for a, b in zip(want, step()))
+
+
+# ---- refusals: on the host, nothing is launched --------------------------------------------------
+def test_refusals():
+    import ctypes
+    from paper_2304_03946_amd import binding as B
+    lib = B.load_library()
+    null, one, odd = ctypes.c_void_p(None), ctypes.c_void_p(16), ctypes.c_void_p(24)
+    big = 1 << 40
+
+    def fwd(A=4, d=64, f=64, E=4, V=4, act=B.SILU, dtype=B.BF16, x=one, w1=one, b1=null, hpre=one, h=null, y=one, ws=one, size=big):
+        return lib.flexmoe_expert_ffn_gated_fwd(x, one, one, w1, b1, one, null, A, d, f, E, V, act, dtype, hpre, h, y, ws, size, null)
+
+    def bwd(A=4, d=64, f=64, E=4, V=4, act=B.SILU, dtype=B.BF16, dy=one, hpre=one, h=null, dx=one, dw1=one, dw2=one, ws=one, size=big):
+        return lib.flexmoe_expert_ffn_gated_bwd(dy, one, hpre, h, one, one, one, one, A, d, f, E, V, act, dtype, dx, dw1, dw2, ws, size,
+                                                null)
+    for call in (fwd, bwd):
+        assert call(act=4) == B.UNSUPPORTED and call(act=-1) == B.UNSUPPORTED and call(dtype=2) == B.UNSUPPORTED
+        for kw in (dict(A=-1), dict(A=1 << 30), dict(d=0), dict(d=12), dict(f=0), dict(f=-8), dict(f=4), dict(f=12), dict(f=1 << 20),
+                   dict(d=1 << 20), dict(f=(1 << 30) + 8), dict(E=0), dict(E=257, V=300), dict(V=3), dict(V=513), dict(ws=null), dict(ws=odd)):
+            assert call(**kw) == B.INVALID_ARG, kw
+        need = B.flexmoe_workspace_bytes(4, 64, 128, 4, 1, 4, B.BF16)
+        assert call(A=64, size=256) == B.WORKSPACE_TOO_SMALL and call(A=4, size=8) == B.WORKSPACE_TOO_SMALL and need > 256
+    for kw in (dict(x=null), dict(x=odd), dict(w1=null), dict(w1=odd), dict(b1=odd), dict(hpre=odd), dict(h=odd), dict(y=null), dict(y=odd)):
+        assert fwd(**kw) == B.INVALID_ARG, kw
+    for kw in (dict(dy=null), dict(hpre=null), dict(hpre=odd), dict(h=odd), dict(dx=null), dict(dx=odd), dict(dw1=null), dict(dw2=odd)):
+        assert bwd(**kw) == B.INVALID_ARG, kw
+    # calls without a gate do not know the new activation
+    assert lib.flexmoe_expert_ffn_fwd(one, one, one, one, null, one, null, 4, 64, 64, 4, 4, B.SILU, B.BF16, one, null, one, one, big,
+                                      null) == B.UNSUPPORTED
