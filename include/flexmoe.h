@@ -187,6 +187,50 @@ int flexmoe_expert_ffn_gated_bwd(const void* dyp, const void* xp, const void* hp
                                  int act, int dtype, void* dxp, void* dw1, void* dw2, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Expert products with 8-bit integers, for serving: symmetric, a scale per output channel of the weights and one per row ("token") of
+ * the activations.  Whole numbers lie in -127 .. 127 and stand for number * scale.  Scales are float.
+ *
+ * flexmoe_quantize_rows: x [M,K] dtype -> q [M,K] int8, scale [M]:
+ *   scale[r] = max(max_k |x[r,k]| / 127, 2^-126) ; q[r,k] = x[r,k] / scale[r] to the nearest whole number, ties to even.
+ *   A row with an infinity or NaN gets the scale NaN and zeros, so whatever is made of it is NaN.
+ * flexmoe_quantize_weights: the same for every output channel of w [E,K,NC] dtype (flexmoe_expert_ffn_fwd's layout)
+ *   -> q [E,NC,K] int8 (the contraction contiguous), scale [E,NC].  Done once per set of weights.
+ * K is a multiple of 16, NC of 8; K < 2^20 (rows), K < 2^17, NC < 2^20 and K * NC < 2^31 (weights, and every call below).
+ */
+int flexmoe_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, void* stream);
+int flexmoe_quantize_weights(const void* w, int E, int K, int NC, int dtype, void* q, float* scale, void* stream);
+
+/* Bytes of scratch for flexmoe_expert_ffn_i8_fwd of these sizes and for flexmoe_expert_matmul_i8 of any K and NC with these N, E, k, V; 0 for
+   sizes that neither takes (the product of d and f serves any f that is a multiple of 8).  Never falls where N alone grows. */
+size_t flexmoe_i8_workspace_bytes(int N, int d, int f, int E, int k, int V, int gated);
+
+/*
+ * Grouped product: y[p,n] = (sum_j xq[r(p),j] * wq[e,n,j]) * xscale[r(p)] * wscale[e,n] + bias[e,n] for the rows p of every bucket v
+ * of expert e, r(p) = src[p] / k, or p where src is NULL.
+ *   xq [N,K] and xscale [N] (src NULL: [N*k,K] and [N*k]), src [N*k] as written by flexmoe_route or NULL, wq [E,NC,K], wscale [E,NC],
+ *   bias [E,NC] dtype or NULL -> y [N*k,NC] dtype.  With E = V = 1 and k = 1 a plain dense product.
+ * The integer sums are exact, so a row's bits depend on nothing but the row, the weights and the bias.
+ */
+int flexmoe_expert_matmul_i8(const void* xq, const float* xscale, const int32_t* src, const int32_t* vexpert_off,
+                             const int32_t* vexpert_owner, const void* wq, const float* wscale, const void* bias, int N, int k, int K,
+                             int NC, int E, int V, int dtype, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Expert FFN forward on 8-bit weights, the permutation folded in: bucket row p is row src[p] / k of x.
+ *   gated = 0:  H = act(x . W1_e + b1_e)            w1q [E,f,d],  w1scale [E,f],  b1 [E,f] or NULL
+ *   gated = 1:  [G | U] = x . W1_e + b1_e, H = act(G) * U    w1q [E,2f,d], w1scale [E,2f], b1 [E,2f] or NULL (G first)
+ *   yp = H . W2_e + b2_e                            w2q [E,d,f],  w2scale [E,d],  b2 [E,d] or NULL
+ *   x [N,d], biases and yp [N*k,d] dtype; src [N*k], vexpert_off [V+1], vexpert_owner [V] as written by flexmoe_route; act: any.
+ * Rows of x are quantised as by flexmoe_quantize_rows, rows of H as
+ *   scale = max(max_j |H[p,j]| / 127, 2^-126) of H in fp32 ; number = (H[p,j] rounded to dtype) / scale to the nearest, ties to even.
+ * d and f are multiples of 16.  Equal calls give equal bits, and a row's bits depend on nothing but the row and its expert's weights.
+ */
+int flexmoe_expert_ffn_i8_fwd(const void* x, const int32_t* src, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1q,
+                              const float* w1scale, const void* b1, const void* w2q, const float* w2scale, const void* b2, int N, int k,
+                              int d, int f, int E, int V, int gated, int act, int dtype, void* yp, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/*
  * Reverse routing and gate-weighted sum, Eq. 4:
  *   y[t,:] = sum_j (topk_w ? topk_w[t*k+j] : 1) * yp[dest[t*k+j], :]
  *   yp [A,d] dtype, dest [A], topk_w [N,k] float or NULL -> y [N,d] dtype (fp32 accumulation).

@@ -24,7 +24,8 @@ EXPORTS = ["flexmoe_status_str", "flexmoe_workspace_bytes", "flexmoe_gate_topk",
            "flexmoe_permute", "flexmoe_expert_ffn_fwd", "flexmoe_expert_ffn_bwd", "flexmoe_combine",
            "flexmoe_gate_bwd", "flexmoe_expert_bias_grads", "flexmoe_expert_ffn_fwd_gather",
            "flexmoe_expert_ffn_fwd_top1", "flexmoe_expert_ffn_bwd_top1", "flexmoe_route_static",
-           "flexmoe_expert_ffn_gated_fwd", "flexmoe_expert_ffn_gated_bwd",
+           "flexmoe_expert_ffn_gated_fwd", "flexmoe_expert_ffn_gated_bwd", "flexmoe_quantize_rows", "flexmoe_quantize_weights",
+           "flexmoe_i8_workspace_bytes", "flexmoe_expert_matmul_i8", "flexmoe_expert_ffn_i8_fwd",
            # host-side scheduler (include/flexmoe_scheduler.h; Python face in scheduler.py)
            "flexmoe_balance_ratio", "flexmoe_step_cost", "flexmoe_make_scheduling_plan", "flexmoe_schedule",
            "flexmoe_placement_table"]
@@ -78,6 +79,16 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.flexmoe_expert_ffn_gated_fwd.argtypes = [c_vp] * 7 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_expert_ffn_gated_bwd.restype = c_int
     lib.flexmoe_expert_ffn_gated_bwd.argtypes = [c_vp] * 8 + [c_int] * 7 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.flexmoe_quantize_rows.restype = c_int
+    lib.flexmoe_quantize_rows.argtypes = [c_vp, c_int, c_int, c_int, c_vp, c_vp, c_vp]
+    lib.flexmoe_quantize_weights.restype = c_int
+    lib.flexmoe_quantize_weights.argtypes = [c_vp, c_int, c_int, c_int, c_int, c_vp, c_vp, c_vp]
+    lib.flexmoe_i8_workspace_bytes.restype = c_sz
+    lib.flexmoe_i8_workspace_bytes.argtypes = [c_int] * 7
+    lib.flexmoe_expert_matmul_i8.restype = c_int
+    lib.flexmoe_expert_matmul_i8.argtypes = [c_vp] * 8 + [c_int] * 7 + [c_vp, c_vp, c_sz, c_vp]
+    lib.flexmoe_expert_ffn_i8_fwd.restype = c_int
+    lib.flexmoe_expert_ffn_i8_fwd.argtypes = [c_vp] * 10 + [c_int] * 9 + [c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_gate_bwd.restype = c_int
     lib.flexmoe_gate_bwd.argtypes = [c_vp] * 10 + [c_int] * 6 + [c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     lib.flexmoe_expert_bias_grads.restype = c_int
@@ -249,6 +260,44 @@ def flexmoe_expert_ffn_gated_bwd(dyp, xp, hpre, w1, w2, vexpert_off, vexpert_own
                                                      dtype_code(xp), _ptr(dxp), _ptr(dw1), _ptr(dw2), _ptr(ws), ws.nbytes,
                                                      _stream())
     _check(st, "flexmoe_expert_ffn_gated_bwd")
+
+
+def flexmoe_quantize_rows(x, q, scale):
+    M, K = x.shape
+    st = load_library().flexmoe_quantize_rows(_ptr(x), M, K, dtype_code(x), _ptr(q), _ptr(scale), _stream())
+    _check(st, "flexmoe_quantize_rows")
+
+
+def flexmoe_quantize_weights(w, q, scale):
+    E, K, NC = w.shape
+    st = load_library().flexmoe_quantize_weights(_ptr(w), E, K, NC, dtype_code(w), _ptr(q), _ptr(scale), _stream())
+    _check(st, "flexmoe_quantize_weights")
+
+
+def flexmoe_i8_workspace_bytes(N, d, f, E, k, V, gated) -> int:
+    return int(load_library().flexmoe_i8_workspace_bytes(N, d, f, E, k, V, gated))
+
+
+def flexmoe_expert_matmul_i8(xq, xscale, src, k, vexpert_off, vexpert_owner, wq, wscale, bias, y, ws):
+    """src None: xq holds a row per bucket row, of y's k per token."""
+    K = xq.shape[1]
+    E, NC, _ = wq.shape
+    V = vexpert_owner.shape[0]
+    N = xq.shape[0] if src is not None else xq.shape[0] // k
+    st = load_library().flexmoe_expert_matmul_i8(_ptr(xq), _ptr(xscale), _ptr(src), _ptr(vexpert_off), _ptr(vexpert_owner),
+                                                 _ptr(wq), _ptr(wscale), _ptr(bias), N, k, K, NC, E, V, dtype_code(y), _ptr(y),
+                                                 _ptr(ws), ws.nbytes, _stream())
+    _check(st, "flexmoe_expert_matmul_i8")
+
+
+def flexmoe_expert_ffn_i8_fwd(x, src, k, vexpert_off, vexpert_owner, w1q, w1scale, b1, w2q, w2scale, b2, gated, act, yp, ws):
+    N, d = x.shape
+    E, _, f = w2q.shape
+    V = vexpert_owner.shape[0]
+    st = load_library().flexmoe_expert_ffn_i8_fwd(_ptr(x), _ptr(src), _ptr(vexpert_off), _ptr(vexpert_owner), _ptr(w1q),
+                                                  _ptr(w1scale), _ptr(b1), _ptr(w2q), _ptr(w2scale), _ptr(b2), N, k, d, f, E, V,
+                                                  int(gated), act, dtype_code(x), _ptr(yp), _ptr(ws), ws.nbytes, _stream())
+    _check(st, "flexmoe_expert_ffn_i8_fwd")
 
 
 def flexmoe_gate_bwd(wg, topk_idx, topk_w, dy, yp, xp, dest, src, vexpert_off, vexpert_owner, dl, dx, dwg, ws):

@@ -264,6 +264,64 @@ int flexmoe_expert_ffn_gated_bwd(const void* dyp, const void* xp, const void* hp
                                           : launch_ffn_gated_bwd_f32(a, dyp, xp, hpre, h, w1, w2, dxp, dw1, dw2, ws, s));
 }
 
+// Integer sums stay below 2^31 where the contraction is shorter than 2^17 (127 * 127 each); a weight matrix is addressed with 32 bits.
+static bool i8_dims_ok(long long K, long long NC, int cols_multiple) {
+  return K >= 16 && K % 16 == 0 && K < (1 << 17) && NC >= cols_multiple && NC % cols_multiple == 0 && NC < kMaxWidth && K * NC < (1ll << 31);
+}
+static bool i8_counts_ok(int N, int k, int E, int V) {
+  return N >= 0 && k >= 1 && k <= FLEXMOE_MAX_TOPK && (long long)N * k < (1ll << 30) && E >= 1 && E <= FLEXMOE_MAX_EXPERTS && V >= E &&
+         V <= FLEXMOE_MAX_VEXPERTS;
+}
+
+size_t flexmoe_i8_workspace_bytes(int N, int d, int f, int E, int k, int V, int gated) {
+  if (!i8_counts_ok(N, k, E, V) || f >= (1 << 17) || !i8_dims_ok(d, gated ? 2ll * f : f, 8)) return 0;      // (f as a product's columns)
+  return i8_ws_bytes(N, d, f, N * k, E, V, true);
+}
+
+int flexmoe_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, void* stream) {
+  if (!dtype_ok(dtype)) return FLEXMOE_UNSUPPORTED;
+  if (M < 0 || M >= (1 << 30) || K < 16 || K % 16 || K >= kMaxWidth) return FLEXMOE_INVALID_ARG;
+  if (M > 0 && (!x || !q || !scale || !aligned16(x) || !aligned16(q) || !aligned16(scale))) return FLEXMOE_INVALID_ARG;
+  return dev_status(launch_quantize_rows(x, M, K, dtype, q, scale, (hipStream_t)stream));
+}
+
+int flexmoe_quantize_weights(const void* w, int E, int K, int NC, int dtype, void* q, float* scale, void* stream) {
+  if (!dtype_ok(dtype)) return FLEXMOE_UNSUPPORTED;
+  if (E < 1 || E > FLEXMOE_MAX_EXPERTS || !i8_dims_ok(K, NC, 8)) return FLEXMOE_INVALID_ARG;
+  if (!w || !q || !scale || !aligned16(w) || !aligned16(q) || !aligned16(scale)) return FLEXMOE_INVALID_ARG;
+  return dev_status(launch_quantize_weights(w, E, K, NC, dtype, q, scale, (hipStream_t)stream));
+}
+
+int flexmoe_expert_matmul_i8(const void* xq, const float* xscale, const int32_t* src, const int32_t* vexpert_off,
+                             const int32_t* vexpert_owner, const void* wq, const float* wscale, const void* bias, int N, int k, int K,
+                             int NC, int E, int V, int dtype, void* y, void* ws, size_t ws_bytes, void* stream) {
+  if (!dtype_ok(dtype)) return FLEXMOE_UNSUPPORTED;
+  if (!i8_counts_ok(N, k, E, V) || !i8_dims_ok(K, NC, 8)) return FLEXMOE_INVALID_ARG;
+  if (!vexpert_off || !vexpert_owner || !ws || !aligned16(ws) || !wq || !wscale || !aligned16(wq) || !aligned16(wscale) || !aligned16(bias))
+    return FLEXMOE_INVALID_ARG;
+  if (N > 0 && (!xq || !xscale || !y || !aligned16(xq) || !aligned16(xscale) || !aligned16(y))) return FLEXMOE_INVALID_ARG;      // src may be NULL
+  const int A = N * k;
+  if (ws_bytes < i8_ws_bytes(N, K, NC, A, E, V, false)) return FLEXMOE_WORKSPACE_TOO_SMALL;
+  const FfnArgs a{A, K, NC, E, V, FLEXMOE_RELU, vexpert_off, vexpert_owner};
+  return dev_status(launch_matmul_i8(a, xq, xscale, src, N, k, wq, wscale, bias, K, NC, dtype, y, ws, (hipStream_t)stream));
+}
+
+int flexmoe_expert_ffn_i8_fwd(const void* x, const int32_t* src, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1q,
+                              const float* w1scale, const void* b1, const void* w2q, const float* w2scale, const void* b2, int N, int k,
+                              int d, int f, int E, int V, int gated, int act, int dtype, void* yp, void* ws, size_t ws_bytes,
+                              void* stream) {
+  if (!dtype_ok(dtype) || !gate_act_ok(act) || (gated != 0 && gated != 1)) return FLEXMOE_UNSUPPORTED;
+  if (!i8_counts_ok(N, k, E, V) || !i8_dims_ok(d, gated ? 2ll * f : f, gated ? 32 : 16) || !i8_dims_ok(f, d, 16)) return FLEXMOE_INVALID_ARG;
+  if (!vexpert_off || !vexpert_owner || !ws || !aligned16(ws) || !w1q || !w2q || !w1scale || !w2scale || !aligned16(w1q) || !aligned16(w2q) ||
+      !aligned16(w1scale) || !aligned16(w2scale) || !aligned16(b1) || !aligned16(b2))
+    return FLEXMOE_INVALID_ARG;
+  if (N > 0 && (!x || !src || !yp || !aligned16(x) || !aligned16(yp))) return FLEXMOE_INVALID_ARG;
+  const int A = N * k;
+  if (ws_bytes < i8_ws_bytes(N, d, f, A, E, V, true)) return FLEXMOE_WORKSPACE_TOO_SMALL;
+  const FfnArgs a{A, d, f, E, V, act, vexpert_off, vexpert_owner};
+  return dev_status(launch_ffn_i8(a, x, src, N, k, w1q, w1scale, b1, w2q, w2scale, b2, gated != 0, dtype, yp, ws, (hipStream_t)stream));
+}
+
 int flexmoe_gate_bwd(const void* wg, const int32_t* topk_idx, const float* topk_w, const void* dy, const void* yp,
                      const void* xp, const int32_t* dest, const int32_t* src, const int32_t* vexpert_off,
                      const int32_t* vexpert_owner, int N, int d, int E, int k, int V, int dtype, float* dl, void* dx,

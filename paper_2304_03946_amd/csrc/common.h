@@ -193,6 +193,14 @@ hipError_t launch_ffn_fwd_f32(const FfnArgs& a, const void* xp, const void* w1, 
 hipError_t launch_ffn_bwd_f32(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept,
                               const void* w1, const void* w2, void* dxp, void* dw1, void* dw2,
                               void* ws, hipStream_t s);
+// 8-bit integer experts (ffn_i8.hip)
+size_t i8_ws_bytes(int N, int d, int f, int A, int E, int V, bool ffn);
+hipError_t launch_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, hipStream_t s);
+hipError_t launch_quantize_weights(const void* w, int E, int K, int NC, int dtype, void* q, float* scale, hipStream_t s);
+hipError_t launch_matmul_i8(const FfnArgs& a, const void* xq, const float* xscale, const int32_t* src, int N, int k, const void* wq,
+                            const float* wscale, const void* bias, int K, int NC, int dtype, void* y, void* ws, hipStream_t s);
+hipError_t launch_ffn_i8(const FfnArgs& a, const void* x, const int32_t* src, int N, int k, const void* w1q, const float* w1s, const void* b1,
+                         const void* w2q, const float* w2s, const void* b2, bool gated, int dtype, void* yp, void* ws, hipStream_t s);
 // gated experts: a.f columns of H, w1 [E, d, 2 f], hpre [A, 2 f]; ws as for a layer of 2 f
 hipError_t launch_ffn_gated_fwd_bf16(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
                                      void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s);

@@ -344,6 +344,9 @@ __device__ __forceinline__ void gate_f32(float z, int act, float* a, float* da) 
     const float s = 1.f / (1.f + expf(-z));
     *a = z * s;
     *da = s * (1.f + z * (1.f - s));
+  } else if (act == FLEXMOE_RELU) {                  // (keeps a NaN)
+    *a = z < 0.f ? 0.f : z;
+    *da = z > 0.f ? 1.f : 0.f;
   } else {
     *a = act_apply(z, act);
     *da = act_deriv(z, act);

@@ -35,6 +35,9 @@ template <int ACT> __device__ __forceinline__ void gate_act(float z, float* a, f
     const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
     *a = z * s;
     *da = fmaf(*a, 1.f - s, s);
+  } else if (ACT == FLEXMOE_RELU) {                      // (keeps a NaN)
+    *a = z < 0.f ? 0.f : z;
+    *da = z > 0.f ? 1.f : 0.f;
   } else {
     act_both<ACT>(z, a, da);
   }
