@@ -160,10 +160,12 @@ int flexmoe_expert_ffn_bwd_top1(const void* dyp, const void* xp, const void* hpr
  *   [G | U] = xp[rows_v,:] . W1_e + b1_e ;  H = act(G) * U ;  yp[rows_v,:] = H . W2_e + b2_e
  *   xp [A,d], w1 [E,d,2f] (columns 0..f-1 give G, f..2f-1 give U), b1 [E,2f] or NULL, w2 [E,f,d], b2 [E,d] or NULL, all dtype;
  *   vexpert_off [V+1], vexpert_owner [V] as written by flexmoe_route.
- *   -> hpre [A,2f] dtype ([G | U], for the backward pass) or NULL (inference: not stored, yp is the same bit for bit),
+ *   -> hpre [A,2f] dtype (for the backward pass) or NULL (inference: not stored, yp is the same bit for bit),
  *      h [A,f] dtype or NULL (H, kept for the backward pass; NULL: in the workspace), yp [A,d] dtype.
- * act: any of flexmoe_act.  H is computed in fp32 from the products' fp32 sums and rounded once, so with bf16 it is not bit for bit what
- * the rounded [G | U] would give.
+ * act: any of flexmoe_act.  H is computed in fp32 from the products' fp32 sums and rounded once.
+ * hpre holds [G | U]: as they are with F32; with BF16 as 16-bit words that keep two mantissa bits more than bf16 where they can (magnitudes
+ * in [2^-20, 2^12): sign, 0, 5 exponent bits counted from 2^-20, 9 mantissa bits; any other: sign, 1, the first 14 bits below the sign of
+ * the fp32 number), each rounded to the nearest.
  * ws: at least flexmoe_workspace_bytes(N, d, 2 * f, E, k, V, dtype) bytes, as for flexmoe_expert_ffn_gated_bwd.
  * d and f are multiples of 8 below 2^20.  Equal calls give equal bits; as in flexmoe_expert_ffn_fwd, a row's last bits may depend on the
  * bucket sizes.
@@ -177,7 +179,7 @@ int flexmoe_expert_ffn_gated_fwd(const void* xp, const int32_t* vexpert_off, con
  *   dH = dyp . W2_e^T ; dG = dH * U * act'(G) ; dU = dH * act(G) ; dHpre = [dG | dU] ; dxp = dHpre . W1_e^T
  *   dw2[e] [f,d] = sum over e's buckets of H_v^T . dyp_v ;  dw1[e] [d,2f] = sum over e's buckets of xp_v^T . dHpre_v
  *   (ascending vExpert id, fp32 accumulation; overwritten, zeros for experts without tokens)
- *   hpre [A,2f] as the forward call left it.  h [A,f]: H as the forward call left it, or NULL: computed again from hpre (with bf16 from
+ *   hpre [A,2f] as the forward call left it.  h [A,f]: H as the forward call left it, or NULL: computed again from hpre (with BF16 from
  *   rounded values, so dw2 then differs by that rounding).
  * ws as in the forward call; afterwards dHpre [A,2f] is at its start, and flexmoe_expert_bias_grads called next with 2f in the place of f
  * gives db1 [E,2f] and db2.

@@ -13,8 +13,9 @@
 //  * G, U and H leave through a wave-private LDS patch as bf16 (half of what fp32 patches move): 16 bytes per lane, 64 per row.
 //  * three sets of kernels, chosen as for an ungated layer with 2 f columns: rows of 256 x 256 tiles with direct-to-LDS loads where K is a
 //    multiple of 128, register-staged ones for other K, and 32- or 64-row tiles for few rows (small_core).
-// Rounding: H is made of the sums before G and U are rounded to bf16 for Hpre (an error of 2^-9 each that y then does not have);
-// the backward pass has only the rounded ones, for act', act and, unless the caller kept H, for H.
+// Rounding: H is made of the fp32 sums and rounded once.  What is kept of G and U for the backward pass are 16-bit words with two mantissa
+// bits more than bf16 has (keep4): as bf16 they put as much error into the gradients as the rounding of dHpre that cannot be
+// avoided (rel. error of dW1 and dX, 64-bit formula: 0.0030 with bf16 words, 0.0024 with these, 0.0017 is the rounding of the output alone).
 //
 // What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.
 #include <algorithm>
@@ -43,6 +44,40 @@ template <int ACT> __device__ __forceinline__ void gate_act(float z, float* a, f
   }
 }
 
+// ---- kept words --------------------------------------------------------------------------------
+// Magnitudes in [2^-20, 2^12) -- all but a few of a layer's -- as sign, 0, 5 exponent and 9 mantissa bits: bits 27 .. 14 of the fp32 number
+// less 2^-20's exponent.  Anything else as sign, 1, and the 14 bits below the sign (8 exponent, 6 mantissa bits), so that nothing overflows or
+// vanishes, zeros, infinities and NaN included.  Either way rounded to the nearest.
+constexpr uint32_t kKeepBase = (127u - 20u) << 23;
+// of the first kind: the sum that holds the word in bits 31 and 27 .. 14; bits 30 .. 28 are zero if the number is of that kind
+__device__ __forceinline__ uint32_t keep_sum(float a) { return __float_as_uint(a) + (0x2000u - kKeepBase); }
+__device__ __forceinline__ uint32_t keep_pair(uint32_t lo, uint32_t hi) {      // two such sums' words
+  const uint32_t low = ((lo >> 14) & 0x3fffu) | ((hi << 2) & 0x3fff0000u);
+  return low | (__builtin_amdgcn_perm(hi, lo, 0x07060302u) & 0x80008000u);
+}
+__device__ __forceinline__ uint32_t keep_any(float a) {
+  const uint32_t u = __float_as_uint(a), m = u & 0x7fffffffu, first = m + (0x2000u - kKeepBase);
+  const uint32_t other = m > 0x7f800000u ? 0x7fffu : 0x4000u | min((m + 0xffffu + ((m >> 17) & 1u)) >> 17, 0x3fc0u);
+  return ((u >> 16) & 0x8000u) | (first >> 28 ? other : first >> 14);
+}
+constexpr uint32_t kKeepOther = 0x70000000u;
+__device__ __forceinline__ uint2 keep4(const float* v) {
+  const uint32_t k[4] = {keep_sum(v[0]), keep_sum(v[1]), keep_sum(v[2]), keep_sum(v[3])};
+  if ((k[0] | k[1] | k[2] | k[3]) & kKeepOther)
+    return make_uint2(keep_any(v[0]) | keep_any(v[1]) << 16, keep_any(v[2]) | keep_any(v[3]) << 16);
+  return make_uint2(keep_pair(k[0], k[1]), keep_pair(k[2], k[3]));
+}
+__device__ __forceinline__ float kept_low(uint32_t w) {
+  const uint32_t m = w & 0x3fffu;
+  return __uint_as_float((w << 16 & 0x80000000u) | (w & 0x4000u ? m << 17 : (m << 14) + kKeepBase));
+}
+__device__ __forceinline__ void kept4(uint2 w, float* v) {
+  v[0] = kept_low(w.x);
+  v[1] = kept_low(w.x >> 16);
+  v[2] = kept_low(w.y);
+  v[3] = kept_low(w.y >> 16);
+}
+
 struct GatedArgs {
   const bf16_t* in;              // fwd: Xp, dH: dYp
   const bf16_t* w;               // fwd: W1 [E, d, 2 f], dH: W2 [E, f, d]
@@ -50,8 +85,8 @@ struct GatedArgs {
   const int32_t* voff;
   const int32_t* owner;
   int V, K, f, row_tiles_max, col_tiles;
-  const bf16_t* hpre_in;         // dH: Hpre [A, 2 f]
-  bf16_t* out0;                  // fwd: Hpre or null, dH: dHpre [A, 2 f]
+  const bf16_t* hpre_in;         // dH: Hpre [A, 2 f], kept words
+  bf16_t* out0;                  // fwd: Hpre (kept words) or null, dH: dHpre [A, 2 f]
   bf16_t* out1;                  // fwd: H [A, f], dH: H or null (kept by the forward pass)
   int act;
 };
@@ -85,7 +120,7 @@ struct DmaSrcGate {
 // Forward.  The wave's accumulators acc[i][0] (G) and acc[i][1] (U) hold 128 rows x 32 columns, 16 x 16 tiles [2 si + sj]: lane L has row
 // 16 si + L % 16, columns 16 sj + 4 (L / 16) .. .  16 rows at a time go through the patch: three [16][32] bf16 tiles (64-byte rows, chunk
 // index XOR row / 4: writes and reads free of bank conflicts), read back as 16 bytes per lane.
-template <int ACT, bool FULL>
+template <int ACT, bool KEEP, bool FULL>
 __device__ __forceinline__ void gated_fwd_rounds(lds_byte_t* patch, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wm, int c0) {
   const int lane = opaque_tid() & 63;
   const int r = lane & 15, g4 = lane >> 4;
@@ -105,36 +140,65 @@ __device__ __forceinline__ void gated_fwd_rounds(lds_byte_t* patch, const DmaAcc
   const uint32_t read_at = srow * 64 + ((ch ^ (srow >> 2)) << 4);
   const int col = c0 + ch * 8;
   const bool col_ok = FULL || col < f;
-  bf16_t* const pre_t = p.out0 ? p.out0 + (size_t)t.row0 * 2 * f + col : nullptr;
+  bf16_t* const pre_t = KEEP ? p.out0 + (size_t)t.row0 * 2 * f + col : nullptr;
+  uint32_t at[2];                                        // where the lane's four columns of a 16 x 16 tile go
+#pragma unroll
+  for (int sj = 0; sj < 2; ++sj) at[sj] = r * 64 + (((sj * 2 + (g4 >> 1)) ^ (r >> 2)) << 4) + (g4 & 1) * 8;
   bf16_t* const h_t = p.out1 + (size_t)t.row0 * f + col;
   const uint32_t row_first = wm * 32 + srow;             // of the tile, round (0, 0)
 #pragma unroll
   for (int round = 0; round < 2 * MB; ++round) {
     const int i = round >> 1, sub = round & 1;
+    typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
+    float gu[2][2][4];                                   // [G, U][sj]
+    uint32_t other = 0;
 #pragma unroll
     for (int sj = 0; sj < 2; ++sj) {
       const int e = 4 * (2 * sub + sj);
-      float g[4], u[4], h[4], da;
+      float h[4], da;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        g[q] = acc[i][0][e + q] + bg[sj][q];
-        u[q] = acc[i][1][e + q] + bu[sj][q];
-        gate_act<ACT>(g[q], &h[q], &da);
-        h[q] *= u[q];
+        gu[0][sj][q] = acc[i][0][e + q] + bg[sj][q];
+        gu[1][sj][q] = acc[i][1][e + q] + bu[sj][q];
+        gate_act<ACT>(gu[0][sj][q], &h[q], &da);
+        h[q] *= gu[1][sj][q];
+        if (KEEP) other |= keep_sum(gu[0][sj][q]) | keep_sum(gu[1][sj][q]);
       }
-      const uint32_t at = r * 64 + (((sj * 2 + (g4 >> 1)) ^ (r >> 2)) << 4) + (g4 & 1) * 8;
-      typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
-      *(lds_u32x2*)(patch + at) = u32x2_t{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])};
-      *(lds_u32x2*)(patch + 1024 + at) = u32x2_t{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3])};
-      *(lds_u32x2*)(patch + 2048 + at) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+      *(lds_u32x2*)(patch + 2048 + at[sj]) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+    }
+    if (KEEP) {
+      uint32_t w[2][2][2];
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+        for (int sj = 0; sj < 2; ++sj)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) w[t2][sj][q] = keep_pair(keep_sum(gu[t2][sj][2 * q]), keep_sum(gu[t2][sj][2 * q + 1]));
+      if (__builtin_expect(other & kKeepOther, 0)) {     // (rare, and one branch for 16 words)
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+          for (int sj = 0; sj < 2; ++sj)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) w[t2][sj][q] = keep_any(gu[t2][sj][2 * q]) | keep_any(gu[t2][sj][2 * q + 1]) << 16;
+      }
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+        for (int sj = 0; sj < 2; ++sj) *(lds_u32x2*)(patch + 1024 * t2 + at[sj]) = u32x2_t{w[t2][sj][0], w[t2][sj][1]};
     }
     asm volatile("" ::: "memory");                       // (a wave's LDS instructions execute in order)
     typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4;
-    const u32x4_t vg = *(lds_u32x4*)(patch + read_at), vu = *(lds_u32x4*)(patch + 1024 + read_at), vh = *(lds_u32x4*)(patch + 2048 + read_at);
+    u32x4_t vg, vu;
+    if (KEEP) {
+      vg = *(lds_u32x4*)(patch + read_at);
+      vu = *(lds_u32x4*)(patch + 1024 + read_at);
+    }
+    const u32x4_t vh = *(lds_u32x4*)(patch + 2048 + read_at);
     asm volatile("" ::: "memory");
     const uint32_t row = row_first + i * 64 + sub * 16;
     if (FULL || (col_ok && (int)row < t.rows_valid)) {
-      if (pre_t) {
+      if (KEEP) {
         bf16_t* o = pre_t + (size_t)row * 2 * f;
         store_nt16(o, vg);
         store_nt16(o + f, vu);
@@ -145,13 +209,13 @@ __device__ __forceinline__ void gated_fwd_rounds(lds_byte_t* patch, const DmaAcc
 }
 
 // dH: the wave's accumulators are 128 rows x 64 columns of dH, rounds and fp32 patch as in epilogue_rounds8.  The side inputs G and U are
-// requested a round ahead.
+// requested two rounds ahead: a load behind a round's stores returns after them.
 template <int ACT, bool KEPT, bool FULL>
 __device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wm, int col_base) {
   const int lane = opaque_tid() & 63;
   const int rsub = lane >> 4, c = lane & 15;
   const int f = p.f;
-  constexpr int kRounds = MB * 2, kIts = 4, kAhead = 1;
+  constexpr int kRounds = MB * 2, kIts = 4, kAhead = 2;
   const int col = col_base + jh * 64 + c * 4;            // of H
   const bool col_ok = FULL || col < f;
   const size_t tile_at = (size_t)t.row0 * 2 * f + col;
@@ -204,8 +268,8 @@ __device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaA
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
       float g[4], u[4], dh[4] = {v[it].x, v[it].y, v[it].z, v[it].w}, dg[4], du[4], h[4];
-      unpack4(sg[round % (kAhead + 1)][it], g);
-      unpack4(su[round % (kAhead + 1)][it], u);
+      kept4(sg[round % (kAhead + 1)][it], g);
+      kept4(su[round % (kAhead + 1)][it], u);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float a, da;
@@ -231,8 +295,13 @@ __device__ __forceinline__ void gated_epilogue(unsigned char* stage, const DmaAc
   unsigned char* patch = stage + wave * 4096;
   if (EPI == EPI_FWD1) {
     const int c0 = t.n0 + (dma_wave_cb0(wave) >> 1) * 32;
-    if (t.rows_valid == BM && t.n0 + GN <= p.f) gated_fwd_rounds<ACT, true>((lds_byte_t*)patch, acc, p, t, wm, c0);
-    else gated_fwd_rounds<ACT, false>((lds_byte_t*)patch, acc, p, t, wm, c0);
+    const bool full = t.rows_valid == BM && t.n0 + GN <= p.f;
+    if (p.out0) {
+      if (full) gated_fwd_rounds<ACT, true, true>((lds_byte_t*)patch, acc, p, t, wm, c0);
+      else gated_fwd_rounds<ACT, true, false>((lds_byte_t*)patch, acc, p, t, wm, c0);
+    } else {
+      gated_fwd_rounds<ACT, false, false>((lds_byte_t*)patch, acc, p, t, wm, c0);
+    }
   } else {
     const int col_base = t.n0 + wn * (NB * 32);
     if (t.rows_valid == BM && t.n0 + BN <= p.f) gated_dh_rounds<ACT, EPI == EPI_DHQ, true>((float*)patch, hh, acc, p, t, wm, col_base);
@@ -352,16 +421,16 @@ __device__ __forceinline__ void gated_direct(const f32x16 (&acc)[MB][NB], const 
             h[q] *= u[q];
           }
           if (p.out0) {
-            *(uint2*)(p.out0 + grow * 2 * f + col) = pack4(z[0], z[1], z[2], z[3]);
-            *(uint2*)(p.out0 + grow * 2 * f + f + col) = pack4(u[0], u[1], u[2], u[3]);
+            *(uint2*)(p.out0 + grow * 2 * f + col) = keep4(z);
+            *(uint2*)(p.out0 + grow * 2 * f + f + col) = keep4(u);
           }
           *(uint2*)(p.out1 + grow * f + col) = pack4(h[0], h[1], h[2], h[3]);
         } else {
           const int col = t.n0 + (wn * NB + j) * 32 + in_blk;
           if (col >= f) continue;
           float z[4], u[4], dg[4], du[4], h[4];
-          unpack4(*(const uint2*)(p.hpre_in + grow * 2 * f + col), z);
-          unpack4(*(const uint2*)(p.hpre_in + grow * 2 * f + f + col), u);
+          kept4(*(const uint2*)(p.hpre_in + grow * 2 * f + col), z);
+          kept4(*(const uint2*)(p.hpre_in + grow * 2 * f + f + col), u);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const float dh = acc[i][j][4 * g + q];
@@ -450,8 +519,9 @@ template <int BM, int EPI> struct GatedSmallPol {
           h[q] *= u[q];
         }
         if (p.out0) {
-          *(uint2*)(p.out0 + row * 2 * f + col) = pack4(g[0], g[1], g[2], g[3]);
-          *(uint2*)(p.out0 + row * 2 * f + f + col) = pack4(u[0], u[1], u[2], u[3]);
+          const float vg[4] = {g[0], g[1], g[2], g[3]}, vu[4] = {u[0], u[1], u[2], u[3]};
+          *(uint2*)(p.out0 + row * 2 * f + col) = keep4(vg);
+          *(uint2*)(p.out0 + row * 2 * f + f + col) = keep4(vu);
         }
         *(uint2*)(p.out1 + row * f + col) = pack4(h[0], h[1], h[2], h[3]);
       } else {
@@ -460,8 +530,8 @@ template <int BM, int EPI> struct GatedSmallPol {
           const int col = n0 + wave * 32 + j * 16 + fg * 4;
           if (col >= f) continue;
           float g[4], u[4], dg[4], du[4], h[4];
-          unpack4(*(const uint2*)(p.hpre_in + row * 2 * f + col), g);
-          unpack4(*(const uint2*)(p.hpre_in + row * 2 * f + f + col), u);
+          kept4(*(const uint2*)(p.hpre_in + row * 2 * f + col), g);
+          kept4(*(const uint2*)(p.hpre_in + row * 2 * f + f + col), u);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const float dh = acc[i][j][q];

@@ -97,6 +97,17 @@ def backward64(dy, x, hpre, h, w1, w2, rows, act, u=0.0):
     return out, dz, ndz
 
 
+def decode(hpre):
+    """[G | U] from the words that the bf16 call keeps, in 64 bits: sign, 0, 5 exponent bits from 2^-20 on and 9 mantissa bits, or sign, 1 and
+    the 14 bits below the sign of an fp32 number."""
+    if hpre.dtype == torch.float32:
+        return hpre.double()
+    w = hpre.view(torch.int16).int() & 0xffff
+    m = w & 0x3fff
+    value = torch.where((w & 0x4000) != 0, m << 17, (m << 14) + ((127 - 20) << 23)).view(torch.float32).double()
+    return torch.where((w & 0x8000) != 0, -value, value)
+
+
 def buckets(counts, E, seed=0):
     """counts: rows per vExpert; owners: every expert once, then the rest at random, shuffled."""
     rng = np.random.default_rng(seed)
@@ -146,11 +157,11 @@ class Case:
         _b().flexmoe_expert_ffn_gated_bwd(self.dy, self.x, self.hpre, self.w1, self.w2, self.voff, self.owner, self.code, self.dxp,
                                           self.dw1, self.dw2, self.ws, h=self.h if kept else None)
 
-    def close(self, name, got, want, noise):
-        u = torch.finfo(self.dt).eps / 2
+    def close(self, name, got, want, noise, u=None):
+        u = torch.finfo(self.dt).eps / 2 if u is None else u
         err, tol = (got.double() - want).abs(), u * want.abs() + (1 + u) * noise + 1e-37
         worst = float((err / tol).max()) if err.numel() else 0.0
-        assert worst <= 1 + 2 * u, f"{name}: {worst:.3f} of the tolerance"
+        assert worst <= 1 + 2 * float(torch.as_tensor(u).max()), f"{name}: {worst:.3f} of the tolerance"
 
     def u(self):
         return torch.finfo(self.dt).eps / 2
@@ -158,11 +169,16 @@ class Case:
     def check_fwd(self):
         b1, b2 = (None, None) if self.b1 is None else (self.b1.double(), self.b2.double())
         out = forward64(self.x.double(), self.w1.double(), b1, self.w2.double(), b2, self.rows, self.act, self.u())
-        for name, got in (("hpre", self.hpre), ("h", self.h), ("y", self.y)):
+        # kept words: 9 mantissa bits, or 6 outside [2^-20, 2^12) (or beside it: the noise)
+        want, noise = out["hpre"]
+        usual = (want.abs() - noise >= 2.0 ** -20) & (want.abs() + noise < 2.0 ** 12)
+        u = 2.0 ** -24 if self.dt == torch.float32 else torch.where(usual, 2.0 ** -10, 2.0 ** -7).double()
+        self.close("hpre", decode(self.hpre), want, noise, u)
+        for name, got in (("h", self.h), ("y", self.y)):
             self.close(name, got, *out[name])
 
     def backward64(self, kept):
-        return backward64(self.dy.double(), self.x.double(), self.hpre.double(), self.h.double() if kept else None, self.w1.double(),
+        return backward64(self.dy.double(), self.x.double(), decode(self.hpre), self.h.double() if kept else None, self.w1.double(),
                           self.w2.double(), self.rows, self.act, self.u())
 
     def check_bwd(self, kept):
@@ -245,6 +261,27 @@ def test_bias_gradients(A, d, f, dtype):
         dz, dy = dz_all[sel], c.dy.double()[sel]
         c.close("db1", db1[e], dz.sum(0), SPREAD * (norm(ndz[sel]) + sums(A) * norm(dz)))
         c.close("db2", db2[e], dy.sum(0), SPREAD * sums(A) * norm(dy))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("A,d,f", [(40, 64, 72), (7300, 2048, 1024), (7400, 2056, 1032)])
+@pytest.mark.parametrize("scale", [0.0, 1e-30, 1e-6, 3e-4, 1.0, 3e3, 1e20])
+def test_kept_words_at_every_magnitude(A, d, f, scale):
+    """G and U of tiny, huge and zero rows: nothing overflows or vanishes on the way to the backward pass."""
+    c = Case(A, d, f, 2, 3, "bf16", "silu", False, seed=8)
+    c.x.mul_(scale)
+    c.x[::3] *= 0.01
+    c.fwd()
+    out = forward64(c.x.double(), c.w1.double(), None, c.w2.double(), None, c.rows, "silu", c.u())
+    want, noise = out["hpre"]
+    usual = (want.abs() - noise >= 2.0 ** -20) & (want.abs() + noise < 2.0 ** 12)
+    # (smallest fp32 numbers: sums of subnormal products, absolute)
+    c.close("hpre", decode(c.hpre), want, noise + 2.0 ** -126, torch.where(usual, 2.0 ** -10, 2.0 ** -7).double())
+    if scale == 0.0:
+        assert not decode(c.hpre).any() and not c.y.any()
+    if scale <= 3e3:
+        c.bwd()
+        c.check_bwd(True)
 
 
 @pytest.mark.gpu
