@@ -79,6 +79,9 @@ struct SmallPlan {
   int* counters;
   int bm;                        // 0: the product does not use these kernels
   int parts;                     // waves that write a bucket's rows
+  const int32_t* src = nullptr;  // gathered products: position -> src[bucket row] / k goes to tokmap; or null
+  int k = 1;
+  int32_t* tokmap = nullptr;
 };
 __device__ __forceinline__ void small_plan_block(const int32_t* __restrict__ voff, const int32_t* __restrict__ owner, int E, int V,
                                                  const SmallPlan& plan, int block, int nblocks) {
@@ -165,7 +168,10 @@ __device__ __forceinline__ void small_plan_block(const int32_t* __restrict__ vof
   constexpr int kWaves = kGemmThreads / kWave;
   for (int w = (block - 1) * kWaves + wave; w < V * plan.parts; w += (nblocks - 1) * kWaves) {
     const int v = w / plan.parts, lo = off[v], len = bucket[v].y, to = pos0[v];
-    for (int i = w % plan.parts * kWave + lane; i < len; i += plan.parts * kWave) plan.rowmap[to + i] = lo + i;
+    for (int i = w % plan.parts * kWave + lane; i < len; i += plan.parts * kWave) {
+      plan.rowmap[to + i] = lo + i;
+      if (plan.src) plan.tokmap[to + i] = plan.src[lo + i] / plan.k;
+    }
   }
 }
 static __global__ __launch_bounds__(kGemmThreads) void small_plan_kernel(const int32_t* __restrict__ voff,

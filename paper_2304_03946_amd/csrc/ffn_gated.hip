@@ -548,15 +548,16 @@ template <int BM, int EPI> struct GatedSmallPol {
       }
     }
   }
+  __device__ __forceinline__ int before(const SmallTile&, const int32_t*, int, int, int, int) const { return 0; }
   template <int RB>
-  __device__ __forceinline__ void epilogue(const f32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg) const {
+  __device__ __forceinline__ void epilogue(const f32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg, int) const {
     FLEXMOE_BY_ACT(p.act, (out<ACT, RB>(acc, t, orow, n0, wave, fr, fg)))
   }
 };
 template <int BM, int EPI> __global__ __launch_bounds__(kSmallThreads, 2) void gated_small_bf16(const SmallCore c, const GatedArgs p) {
-  __shared__ __align__(1024) unsigned char smem[SmallCfg<BM>::kLds];
+  __shared__ __align__(1024) unsigned char smem[CoreCfg<BM, SN>::kLds];
   const GatedSmallPol<BM, EPI> pol{p};
-  small_core<BM, EPI != EPI_FWD1, EPI == EPI_FWD1, f32x4>(c, pol, smem, blockIdx.x, gridDim.x);
+  small_core<BM, SN, EPI != EPI_FWD1, EPI == EPI_FWD1, f32x4>(c, pol, smem, blockIdx.x, gridDim.x);
 }
 
 // ---- host ----------------------------------------------------------------------------------------
@@ -571,7 +572,7 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
               (const bf16_t*)hpre_in, (bf16_t*)out0, (bf16_t*)out1, a.act};
   if (rk.small.bm) {
     const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, K, FWD ? 2 * f : f, FWD ? (f + SN / 2 - 1) / (SN / 2) : (f + SN - 1) / SN,
-                      nullptr, 1, rk.small_partial, rk.small.counters};
+                      rk.small.rowmap, rk.small_partial, rk.small.counters};
     const long long most = ((long long)a.A / rk.small.bm + a.E) * c.col_tiles * kSmallSplitMax;
     const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
     if (rk.small.bm == 32) hipLaunchKernelGGL((gated_small_bf16<32, EPI>), grid, dim3(kSmallThreads), 0, s, c, p);

@@ -378,27 +378,42 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
 }
 
 // Few rows, or K in no whole rounds of the kernel above.
-template <int EPI, typename T> struct I8SmallPol {
+template <int RB> struct I8Ahead {
+  float rs[RB], cs[2][4], b[2][4];      // scales of the lane's rows and columns, biases
+};
+template <int RB, int EPI, typename T> struct I8SmallPol {
   const I8Args& p;
-  template <int ACT, int RB>
-  __device__ __forceinline__ void out(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg) const {
+  __device__ __forceinline__ I8Ahead<RB> before(const SmallTile& t, const int32_t* inmap, int n0, int wave, int fr, int fg) const {
     constexpr bool GATE = EPI == I8_GATE;
     const int NC = p.NC, wcols = GATE ? 2 * NC : NC;
-    float cs[2][4], b[2][4] = {};
-    bool ok[2];
+    I8Ahead<RB> v;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) v.rs[i] = p.xscale[inmap[t.first + min(i * 16 + fr, t.rows - 1)]];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int col = n0 + (GATE ? wave * 16 : wave * 32 + j * 16) + fg * 4;
-      ok[j] = col < NC;
       const size_t at = (size_t)t.e * wcols + min(col, NC - 4) + (GATE && j ? NC : 0);
-      load4(p.wscale + at, cs[j]);
-      if (p.bias) load4((const T*)p.bias + at, b[j]);
+      load4(p.wscale + at, v.cs[j]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v.b[j][q] = 0.f;
+      if (p.bias) load4((const T*)p.bias + at, v.b[j]);
     }
+    return v;
+  }
+  template <int ACT>
+  __device__ __forceinline__ void out(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
+                                      const I8Ahead<RB>& v) const {
+    constexpr bool GATE = EPI == I8_GATE;
+    const int NC = p.NC;
+    const float(&cs)[2][4] = v.cs, (&b)[2][4] = v.b;
+    bool ok[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) ok[j] = n0 + (GATE ? wave * 16 : wave * 32 + j * 16) + fg * 4 < NC;
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
       const bool there = i * 16 + fr < t.rows;           // (all lanes take part in the maximum)
       const int row = orow[i];
-      const float rs = p.xscale[p.gsrc ? p.gsrc[row] / p.gk : row];
+      const float rs = v.rs[i];
       float z[2][4];
       uint32_t most = 0;
 #pragma unroll
@@ -426,16 +441,18 @@ template <int EPI, typename T> struct I8SmallPol {
       }
     }
   }
-  template <int RB>
-  __device__ __forceinline__ void epilogue(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg) const {
-    if constexpr (EPI == I8_OUT) out<FLEXMOE_RELU, RB>(acc, t, orow, n0, wave, fr, fg);
-    else FLEXMOE_I8_BY_ACT(p.act, (out<ACT, RB>(acc, t, orow, n0, wave, fr, fg)))
+  __device__ __forceinline__ void epilogue(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
+                                           const I8Ahead<RB>& v) const {
+    if constexpr (EPI == I8_OUT) out<FLEXMOE_RELU>(acc, t, orow, n0, wave, fr, fg, v);
+    else FLEXMOE_I8_BY_ACT(p.act, out<ACT>(acc, t, orow, n0, wave, fr, fg, v))
   }
 };
+// columns of a tile (see small_core): row tiles of 16 rows have 64
+template <int BM> constexpr int i8_cols() { return BM == 64 ? 128 : 64; }
 template <int BM, int EPI, typename T> __global__ __launch_bounds__(kSmallThreads, 2) void i8_small(const SmallCore c, const I8Args p) {
-  __shared__ __align__(1024) unsigned char smem[SmallCfg<BM>::kLds];
-  const I8SmallPol<EPI, T> pol{p};
-  small_core<BM, true, EPI == I8_GATE, i32x4>(c, pol, smem, blockIdx.x, gridDim.x);
+  __shared__ __align__(1024) unsigned char smem[CoreCfg<BM, i8_cols<BM>()>::kLds];
+  const I8SmallPol<BM / 16, EPI, T> pol{p};
+  small_core<BM, i8_cols<BM>(), true, EPI == I8_GATE, i32x4>(c, pol, smem, blockIdx.x, gridDim.x);
 }
 
 // ---- plan: what the products look up, the rows' integers and the zeros of `largest`, in one launch ----------------------
@@ -468,11 +485,11 @@ __global__ __launch_bounds__(kGemmThreads) void i8_prep_kernel(const int32_t* __
 }
 
 // ---- host --------------------------------------------------------------------------------------
-// Workspace: row tiles of the few-rows kernels (room for tiles of 32 rows), row list, counters, partial tiles; table of 256-row
+// Workspace: row tiles of the few-rows kernels (room for tiles of 16 rows), row lists, counters, partial tiles; table of 256-row
 // tiles; and for the FFN integers and scales of x, largest values, scales and integers of H, H.
 struct I8Ws {
   i32x4* small_tab;
-  int32_t* rowmap;
+  int32_t *rowmap, *tokmap;
   int* counters;
   float* partial;
   i32x4* row_tab;
@@ -490,8 +507,9 @@ static size_t i8_layout(char* at, int N, int d, int f, int A, int E, int V, bool
     at += align_up(bytes, 256);
     return p;
   };
-  w->small_tab = (i32x4*)take((size_t)(A / 32 + E + 1) * sizeof(i32x4));
+  w->small_tab = (i32x4*)take((size_t)(A / 16 + E + 1) * sizeof(i32x4));
   w->rowmap = (int32_t*)take((size_t)A * sizeof(int32_t));
+  w->tokmap = (int32_t*)take((size_t)A * sizeof(int32_t));
   w->counters = (int*)take(kSmallSlots * sizeof(int));
   w->partial = (float*)take((size_t)kSmallSlots * 64 * SN * sizeof(float));
   w->row_tab = (i32x4*)take(rows_tab_bytes(A / BM + V));
@@ -514,7 +532,7 @@ size_t i8_ws_bytes(int N, int d, int f, int A, int E, int V, bool ffn) {
 // bf16 kernels (small_rows): per tile both sides do what they do there, on half the bytes and twice the rate.  K in no whole
 // rounds, or gathered rows beyond 32-bit byte offsets: few-rows kernels.
 static int i8_bm(int few, int K, bool gathered, long long rows_in) {
-  if (few) return few;
+  if (few) return few == 32 ? 16 : 64;
   return K % 256 || (gathered && rows_in * K >= (1ll << 31)) ? 64 : 0;
 }
 template <int EPI, typename T>
@@ -522,11 +540,11 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
   constexpr bool GATE = EPI == I8_GATE;
   if (bm) {
     const int wcols = GATE ? 2 * p.NC : p.NC;
-    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, GATE ? (p.NC + SN / 2 - 1) / (SN / 2) : (p.NC + SN - 1) / SN,
-                      p.gsrc, p.gk, w.partial, w.counters};
+    const int cols = bm == 64 ? i8_cols<64>() : i8_cols<16>();
+    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters};
     const long long most = ((long long)a.A / bm + a.E) * c.col_tiles * kSmallSplitMax;
     const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
-    if (bm == 32) hipLaunchKernelGGL((i8_small<32, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);
+    if (bm == 16) hipLaunchKernelGGL((i8_small<16, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);
     else hipLaunchKernelGGL((i8_small<64, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);
     return hipGetLastError();
   }
@@ -544,9 +562,9 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
 
 // few: row tiles the plan is for, 0: none
 template <typename T>
-static void launch_prep(const FfnArgs& a, int bm1, int bm2, I8Prep g, const I8Ws& w, hipStream_t s) {
+static void launch_prep(const FfnArgs& a, int bm1, int bm2, const int32_t* src, int k, I8Prep g, const I8Ws& w, hipStream_t s) {
   const int bm = bm1 ? bm1 : bm2;
-  g.small = SmallPlan{w.small_tab, w.rowmap, w.counters, bm, std::max(1, std::min(a.A / (a.V * 512), 2048 / a.V))};
+  g.small = SmallPlan{w.small_tab, w.rowmap, w.counters, bm, std::max(1, std::min(a.A / (a.V * 512), 2048 / a.V)), src, k, w.tokmap};
   g.small_blocks = bm ? 1 + (a.V * g.small.parts + 3) / 4 : 0;      // as the bf16 kernels' plan
   g.row_tab = bm1 && bm2 ? nullptr : w.row_tab;
   g.row_blocks = g.row_tab ? std::max(1, std::min(64, (a.A / BM + a.V + kGemmThreads - 1) / kGemmThreads)) : 0;
@@ -560,7 +578,7 @@ static hipError_t matmul_i8_t(const FfnArgs& a, const void* xq, const float* xsc
   I8Ws w;
   i8_layout((char*)ws, N, K, NC, a.A, a.E, a.V, false, &w);
   const int bm = i8_bm(rows_kernels(a, nullptr).small.bm, K, src != nullptr, N);
-  launch_prep<T>(a, bm, bm, I8Prep{}, w, s);
+  launch_prep<T>(a, bm, bm, src, k, I8Prep{}, w, s);
   const I8Args p{(const bf16_t*)xq, (const bf16_t*)wq, xscale, wscale, bias, K / 2, NC, 0, src, k, y, nullptr, FLEXMOE_RELU};
   return launch_i8<I8_OUT, T>(a, p, bm, w, s);
 }
@@ -588,7 +606,7 @@ static hipError_t ffn_i8_t(const FfnArgs& a, const void* x, const int32_t* src, 
   g.K = a.d;
   g.q = w.xq;
   g.scale = w.xscale;
-  launch_prep<T>(a, bm1, bm2, g, w, s);
+  launch_prep<T>(a, bm1, bm2, src, k, g, w, s);
   const I8Args p1{(const bf16_t*)w.xq, (const bf16_t*)w1q, w.xscale, w1s, b1, a.d / 2, a.f, 0, src, k, w.h, w.largest, a.act};
   hipError_t err = gated ? launch_i8<I8_GATE, T>(a, p1, bm1, w, s) : launch_i8<I8_ACT, T>(a, p1, bm1, w, s);
   if (err != hipSuccess) return err;

@@ -15,8 +15,11 @@ namespace flexmoe {
 //    Sums of integers are exact: segments change nothing, and a row's bits do not depend on the other rows.
 //  * GATED: the tile's 128 weight columns are 64 columns of the first half (gate) and the same 64 of the second (up), 16 and 16 in
 //    turn, so that a wave holds both values of an output in the same lane: acc[i][0] and acc[i][1].
+//  * COLS: a tile is 128 columns and a stage 128 bytes of k, or (WT) 64 columns and 256 bytes: HBM serves pieces of 256 bytes better than
+//    lines 4 KB and more apart.  With 64 columns two waves share an output block, each with half of a stage's k, and add their sums at
+//    the end.
 //  * rows of `in` are addressed with 64 bits, so any number of rows is served.
-//  * pol.epilogue(acc, tile, ...) does the rest.
+//  * pol.before(...) fetches what the epilogue reads ahead of the K loop, pol.epilogue(acc, tile, ...) does the rest.
 // =============================================================================================
 struct SmallCore {
   const bf16_t* in;              // [rows, K]
@@ -24,37 +27,53 @@ struct SmallCore {
   const i32x4* tab;              // as SmallArgs
   const int32_t* rowmap;
   int K, NC, col_tiles;          // NC: all weight columns (GATED: both halves)
-  const int32_t* gsrc;           // gathered rows of `in`: row gsrc[bucket row] / gk; or null
-  int gk;
+  const int32_t* inmap;          // position in expert order -> row of `in` (rowmap, or gathered rows)
   float* partial;
   int* counters;
 };
 struct SmallTile {
   int first, rows, e, ct;        // position in rowmap, rows, expert, column tile
 };
+template <int BM, int COLS> struct CoreCfg {
+  static constexpr int kKBytes = 16384 / COLS;           // of a row's k in a stage
+  static constexpr int kABytes = BM * kKBytes, kWBytes = 16384;
+  static constexpr int kStage = kABytes + kWBytes;
+  static constexpr int S = 81920 / kStage;               // stages: half of a compute unit's LDS
+  static constexpr int kLds = S * kStage;
+  static constexpr int kALoads = kABytes / 1024 / kSmallWaves, kWLoads = kWBytes / 1024 / kSmallWaves, kLoads = kALoads + kWLoads;
+  static constexpr int kKUnits = kKBytes / 2;            // two-byte units of k in a stage
+  static_assert(kALoads >= 1 && S >= 3 && S <= 4, "small_wait");
+};
+// segments of a contraction: small_segments, in stages of 128 bytes of k
+__host__ __device__ inline int core_segments(int tiles, int k_units) { return small_segments(tiles, (k_units + SK - 1) / SK); }
 
-template <int BM, bool WT, bool GATED, typename V4, typename Pol>
+template <int BM, int COLS, bool WT, bool GATED, typename V4, typename Pol>
 __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, unsigned char* smem, unsigned block, unsigned blocks) {
-  typedef SmallCfg<BM> C;
-  constexpr int S = C::S, RB = BM / 16, NB2 = SN / kSmallWaves / 16;      // 16-row and 16-column blocks of a wave
+  typedef CoreCfg<BM, COLS> C;
+  static_assert(COLS == 128 || (COLS == 64 && WT), "tile");
+  constexpr int S = C::S, RB = BM / 16, NB2 = 2;         // 16-row and 16-column blocks of a wave
+  constexpr int kPer = C::kKBytes / 16, kRows = 64 / kPer;      // 16-byte chunks of a row in a stage, rows of a direct load
+  constexpr int kKWaves = COLS == 64 ? 2 : 1;            // waves that share an output block
+  constexpr int kActive = kSmallThreads / kKWaves;       // threads with outputs
   lds_byte_t* const sm = (lds_byte_t*)smem;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)sm);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const int fr = lane & 15, fg = lane >> 4;              // fragment row (or column), group of 16 bytes of k
   const RowTabPtr tab = (RowTabPtr)p.tab;
+  const int cw = wave % (kSmallWaves / kKWaves), kw = wave / (kSmallWaves / kKWaves);      // the wave's 32 columns, its part of a stage's k
   const int K = p.K, NC = p.NC, half = NC / 2;
   const int rows_act = tab[0][0];
-  const int k_tiles = (K + SK - 1) / SK;
+  const int k_tiles = (K + C::kKUnits - 1) / C::kKUnits;
   const int tiles = rows_act * p.col_tiles;
-  const int nseg = small_segments(tiles, k_tiles);
+  const int nseg = core_segments(tiles, K);
   // without segments: the XCD-aware patch order; with them: tile-major, a tile's segments side by side
   const unsigned total = nseg > 1 ? (unsigned)(tiles * nseg) : patched_grid(rows_act, p.col_tiles);
 
   uint32_t la, lw;                                       // lane parts of the LDS fragment addresses
-  la = fr * 128 + ((fg ^ (fr & 7)) << 4);                // second half of a stage: chunk index XOR 4
+  la = fr * C::kKBytes + ((fg ^ (fr & (kPer - 1))) << 4);      // later 64 bytes of k: chunk index XOR 4, 8, 12
   if (WT) {
-    lw = C::kABytes + wave * (NB2 * 2048) + la;
+    lw = C::kABytes + cw * (NB2 * 16 * C::kKBytes) + la;
   } else {
     const int k = 8 * fg + (fr >> 2);
     const int x = ((fr >> 2) << 2) ^ ((fg & 1) << 1);
@@ -74,26 +93,23 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
     const i32x4 d = tab[1 + rt];
     const SmallTile t{d[0], d[1], d[2], ct};
     // first column of the tile, and columns there are (GATED: of either half)
-    const int n0 = ct * (GATED ? SN / 2 : SN), cols = min(GATED ? SN / 2 : SN, (GATED ? half : NC) - n0);
+    const int n0 = ct * (GATED ? COLS / 2 : COLS), cols = min(GATED ? COLS / 2 : COLS, (GATED ? half : NC) - n0);
     const int kt0 = (int)((long long)k_tiles * seg / nseg), kt1 = (int)((long long)k_tiles * (seg + 1) / nseg);
     const bf16_t* w_e = p.w + (size_t)t.e * K * NC + (WT ? (size_t)n0 * K : (size_t)n0);
 
     // rows of the wave's loads (rows past the tile repeat its last row) and of its outputs
     const bf16_t* aptr[C::kALoads];
-    int akc;                                             // the lane's chunk of a row, in two-byte units
-    {
-      const int lr = lane >> 3;
-      akc = ((lane & 7) ^ lr) * 8;
+    int akc[C::kALoads];                                 // the lane's chunk of a row, in two-byte units
 #pragma unroll
-      for (int q = 0; q < C::kALoads; ++q) {
-        int r = p.rowmap[t.first + min((wave * C::kALoads + q) * 8 + lr, t.rows - 1)];
-        if (p.gsrc) r = p.gsrc[r] / p.gk;
-        aptr[q] = p.in + (size_t)r * K + akc;
-      }
+    for (int q = 0; q < C::kALoads; ++q) {
+      const int row = (wave * C::kALoads + q) * kRows + lane / kPer;
+      akc[q] = ((lane % kPer) ^ (row & (kPer - 1))) * 8;
+      aptr[q] = p.in + (size_t)p.inmap[t.first + min(row, t.rows - 1)] * K + akc[q];
     }
     int orow[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) orow[b] = p.rowmap[t.first + min(b * 16 + fr, t.rows - 1)];
+    const auto ahead = pol.before(t, p.inmap, n0, cw, fr, fg);
     uint32_t woff[C::kWLoads];
     int wk[C::kWLoads];                                  // k (in the stage) of the lane's first element
     size_t wbase[C::kWLoads];                            // (uniform) where the load's rows start behind w_e: GATED && WT, the up half
@@ -102,11 +118,11 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       const int i = wave * C::kWLoads + q;
       wbase[q] = 0;
       if (WT) {
-        int row = i * 8 + (lane >> 3);
-        wk[q] = ((lane & 7) ^ (row & 7)) * 8;
+        int row = i * kRows + lane / kPer;
+        wk[q] = ((lane % kPer) ^ (row & (kPer - 1))) * 8;
         if (GATED) {
           row = (row >> 5) * 16 + (row & 15);
-          if ((i >> 1) & 1) wbase[q] = (size_t)half * K;
+          if (((i * kRows) >> 4) & 1) wbase[q] = (size_t)half * K;
         }
         woff[q] = (uint32_t)((uint32_t)min(row, cols - 1) * (uint32_t)K + wk[q]) * 2;
       } else {
@@ -122,9 +138,9 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
     }
     auto issue = [&](int kt) {
       const unsigned st = lds0 + (unsigned)((kt - kt0) % S) * C::kStage;
-      const int k0 = kt * SK;
+      const int k0 = kt * C::kKUnits;
       const bf16_t* wb = w_e + (WT ? (size_t)k0 : (size_t)k0 * NC);
-      if (k0 + SK <= K) {
+      if (k0 + C::kKUnits <= K) {
 #pragma unroll
         for (int q = 0; q < C::kALoads; ++q) small_load_at(aptr[q] + k0, st + (wave * C::kALoads + q) * 1024);
 #pragma unroll
@@ -132,7 +148,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       } else {                                           // past K: zeros on both sides
         const bf16_t* z = (const bf16_t*)kSmallZero + (lane & 7) * 8;
 #pragma unroll
-        for (int q = 0; q < C::kALoads; ++q) small_load_at(k0 + akc < K ? aptr[q] + k0 : z, st + (wave * C::kALoads + q) * 1024);
+        for (int q = 0; q < C::kALoads; ++q) small_load_at(k0 + akc[q] < K ? aptr[q] + k0 : z, st + (wave * C::kALoads + q) * 1024);
 #pragma unroll
         for (int q = 0; q < C::kWLoads; ++q)
           small_load_at(k0 + wk[q] < K ? (const bf16_t*)((const char*)(wb + wbase[q]) + woff[q]) : z,
@@ -159,11 +175,12 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       const lds_byte_t* st = sm + ((kt - kt0) % S) * C::kStage;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
+        const uint32_t kx = (uint32_t)((kw * 2 + ks) << 6);
         bf16x8 a[RB], w[NB2];
 #pragma unroll
         for (int j = 0; j < NB2; ++j) {
           if (WT) {
-            w[j] = *(const __attribute__((address_space(3))) bf16x8*)(st + (lw ^ (ks << 6)) + j * 2048);
+            w[j] = *(const __attribute__((address_space(3))) bf16x8*)(st + (lw ^ kx) + j * (16 * C::kKBytes));
           } else {
             const lds_byte_t* at = st + (lw ^ (uint32_t)(j << 5)) + ks * (32 * 256);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
@@ -173,7 +190,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
           }
         }
 #pragma unroll
-        for (int i = 0; i < RB; ++i) a[i] = *(const __attribute__((address_space(3))) bf16x8*)(st + (la ^ (ks << 6)) + i * 2048);
+        for (int i = 0; i < RB; ++i) a[i] = *(const __attribute__((address_space(3))) bf16x8*)(st + (la ^ kx) + i * (16 * C::kKBytes));
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -181,22 +198,41 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       }
     }
     __syncthreads();                                     // every wave has left the last stage
+    if (kKWaves == 2) {
+      typedef __attribute__((address_space(3))) V4* Ptr;
+      const Ptr at = (Ptr)sm + (cw * kWave + lane);
+      if (kw == 1) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB2; ++j) at[(i * NB2 + j) * kActive] = acc[i][j];
+      }
+      __syncthreads();
+      if (kw == 0) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB2; ++j) acc[i][j] += at[(i * NB2 + j) * kActive];
+      }
+    }
 
     if (nseg > 1) {
       // partial tiles cross XCDs: see rows_gemm_small_bf16
       const int tile = rt * p.col_tiles + ct;
       typedef unsigned long long u64;
       typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      u64* part = (u64*)(p.partial + (size_t)tile * nseg * (BM * SN));
+      u64* part = (u64*)(p.partial + (size_t)tile * nseg * (BM * COLS));
+      if (kw == 0) {
 #pragma unroll
-      for (int i = 0; i < RB; ++i)
+        for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB2; ++j) {
-          u64* dst = part + (size_t)seg * (BM * SN / 2) + (i * NB2 + j) * (2 * kSmallThreads) + threadIdx.x;
-          const u32x4 bits = __builtin_bit_cast(u32x4, acc[i][j]);
-          __hip_atomic_store(dst, (u64)bits[0] | (u64)bits[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          __hip_atomic_store(dst + kSmallThreads, (u64)bits[2] | (u64)bits[3] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
+          for (int j = 0; j < NB2; ++j) {
+            u64* dst = part + (size_t)seg * (BM * COLS / 2) + (i * NB2 + j) * (2 * kActive) + threadIdx.x;
+            const u32x4 bits = __builtin_bit_cast(u32x4, acc[i][j]);
+            __hip_atomic_store(dst, (u64)bits[0] | (u64)bits[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(dst + kActive, (u64)bits[2] | (u64)bits[3] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          }
+      }
       __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the stores have arrived
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -208,24 +244,26 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       const bool last = __builtin_amdgcn_readfirstlane(*(volatile __attribute__((address_space(3))) int*)sm) == nseg - 1;
       if (!last) continue;
       if (threadIdx.x == 0) p.counters[tile] = 0;        // as the plan left it: the call's next product counts there too
+      if (kw == 0) {
 #pragma unroll
-      for (int i = 0; i < RB; ++i)
+        for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB2; ++j) {
-          V4 s = V4{0, 0, 0, 0};
-          for (int g = 0; g < nseg; ++g) {
-            u64* from = part + (size_t)g * (BM * SN / 2) + (i * NB2 + j) * (2 * kSmallThreads) + threadIdx.x;
-            const u64 lo = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const u64 hi = __hip_atomic_load(from + kSmallThreads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s += __builtin_bit_cast(V4, u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)});
+          for (int j = 0; j < NB2; ++j) {
+            V4 s = V4{0, 0, 0, 0};
+            for (int g = 0; g < nseg; ++g) {
+              u64* from = part + (size_t)g * (BM * COLS / 2) + (i * NB2 + j) * (2 * kActive) + threadIdx.x;
+              const u64 lo = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+              const u64 hi = __hip_atomic_load(from + kActive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+              s += __builtin_bit_cast(V4, u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)});
+            }
+            acc[i][j] = s;
           }
-          acc[i][j] = s;
-        }
+      }
       __syncthreads();                                   // the flag has been read
     }
     // lane: row 16 i + fr of the tile (bucket row orow[i], there if 16 i + fr < rows), four columns from 4 fg on of 16-column block
-    // 2 wave + j (GATED: j = 0 gate, 1 up, of columns n0 + 16 wave + 4 fg ..)
-    pol.epilogue(acc, t, orow, n0, wave, fr, fg);
+    // 2 cw + j (GATED: j = 0 gate, 1 up, of columns n0 + 16 cw + 4 fg ..)
+    if (kw == 0) pol.epilogue(acc, t, orow, n0, cw, fr, fg, ahead);
   }
 }
 
