@@ -65,23 +65,39 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
 template <typename T>
 __device__ __forceinline__ void quantize_row(const T* __restrict__ x, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
   const int lane = threadIdx.x & 63;
+  constexpr int kHeld = 4, kStep = kWave * 16;           // 4096 elements stay in registers; of longer rows the rest is read twice
   uint32_t m = 0;
-  I8Load<T> d;
+  I8Load<T> d[kHeld];
   float v[16];
-  for (int k = lane * 16; k < K; k += kWave * 16) {
-    d.load(x + k);
-    d.get(v);
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c)
+    if (c * kStep + lane * 16 < K) d[c].load(x + c * kStep + lane * 16);
+  auto largest = [&](const I8Load<T>& p) {
+    p.get(v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  };
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c)
+    if (c * kStep + lane * 16 < K) largest(d[c]);
+  for (int k = kHeld * kStep + lane * 16; k < K; k += kStep) {
+    I8Load<T> p;
+    p.load(x + k);
+    largest(p);
   }
   const float s = i8_scale(wave_umax(m)), inv = 1.f / s;
   if (lane == 0) *scale = s;
-  for (int k = lane * 16; k < K; k += kWave * 16) {
-    if (K > kWave * 16) {                                // (else still there)
-      d.load(x + k);
-      d.get(v);
-    }
+  auto out = [&](const I8Load<T>& p, int k) {
+    p.get(v);
     *(uint4*)(q + k) = make_uint4(i8_pack(v, s, inv), i8_pack(v + 4, s, inv), i8_pack(v + 8, s, inv), i8_pack(v + 12, s, inv));
+  };
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c)
+    if (c * kStep + lane * 16 < K) out(d[c], c * kStep + lane * 16);
+  for (int k = kHeld * kStep + lane * 16; k < K; k += kStep) {
+    I8Load<T> p;
+    p.load(x + k);
+    out(p, k);
   }
 }
 constexpr int kQuantWaves = 4;
@@ -193,9 +209,9 @@ struct DmaSrcGateRows {
 // Epilogue of a wave of the 256 x 256 kernel: rounds of 16 rows (row lane % 16 of them, four columns from 4 (lane / 16) on in each 16 x 16
 // tile) in fp32, through a wave-private patch (16-byte chunks, index XOR a part of the row: free of conflicts both ways) to 16 bytes
 // per lane.
-template <int EPI, typename T, int ACT, bool FULL>
+template <int EPI, typename T, int ACT, bool FULL, bool BIAS>
 __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc, const I8Args& p, const RowTile& t, int wave,
-                                          const float* row_scale, uint32_t* row_largest) {
+                                          const float* row_scale, const float* col_scale, uint32_t* row_largest) {
   constexpr bool GATE = EPI == I8_GATE;
   constexpr int kCols = GATE ? 32 : 64, kChunks = kCols * (int)sizeof(T) / 16;      // of the wave's block of outputs
   constexpr int kPer = 16 / (int)sizeof(T);                                         // columns of a chunk
@@ -204,7 +220,8 @@ __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc
   const int wm = dma_wave_wm(wave), cb0 = dma_wave_cb0(wave);
   const int NC = p.NC, c0 = t.n0 + (GATE ? (cb0 >> 1) * 32 : cb0 * 32);
   const int wcols = GATE ? 2 * NC : NC;
-  float cs[2][2][4], b[2][2][4] = {};
+  const float* const cs_at = col_scale + cb0 * 32 + 4 * g4;
+  float b[2][2][4] = {};
   bool ok[2][2];
 #pragma unroll
   for (int jj = 0; jj < 2; ++jj)
@@ -212,9 +229,7 @@ __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc
     for (int sj = 0; sj < 2; ++sj) {
       const int col = c0 + (GATE ? 0 : 32 * jj) + 16 * sj + 4 * g4;
       ok[jj][sj] = FULL || col < NC;
-      const size_t at = (size_t)t.e * wcols + min(col, NC - 4) + (GATE && jj ? NC : 0);
-      load4(p.wscale + at, cs[jj][sj]);
-      if (p.bias) load4((const T*)p.bias + at, b[jj][sj]);
+      if (BIAS) load4((const T*)p.bias + (size_t)t.e * wcols + min(col, NC - 4) + (GATE && jj ? NC : 0), b[jj][sj]);
     }
   auto swz_of = [](int row) { return kChunks == 4 ? (row >> 2) & 3 : kChunks == 8 ? (row >> 1) & 7 : row & 15; };
 #pragma unroll
@@ -228,9 +243,12 @@ __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc
       const int e = 4 * (2 * sub + sj);
       float z[2][4];
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj)
+      for (int jj = 0; jj < 2; ++jj) {
+        const float4 cs = *(const float4*)(cs_at + 32 * jj + 16 * sj);
+        const float c4[4] = {cs.x, cs.y, cs.z, cs.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) z[jj][q] = fmaf((float)acc[i][jj][e + q], rs * cs[jj][sj][q], b[jj][sj][q]);
+        for (int q = 0; q < 4; ++q) z[jj][q] = fmaf((float)acc[i][jj][e + q], rs * c4[q], b[jj][sj][q]);
+      }
 #pragma unroll
       for (int jj = 0; jj < (GATE ? 1 : 2); ++jj) {
         float o[4];
@@ -283,7 +301,7 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
   __shared__ __align__(1024) unsigned char stage1[kDmaStageBytes];
   __shared__ __align__(1024) unsigned char stage2[kDmaStageBytes];
   __shared__ __align__(1024) unsigned char stage3[kDmaStageBytes];
-  __shared__ float row_scale[BM];
+  __shared__ __align__(16) float row_scale[BM], col_scale[BN];
   __shared__ uint32_t row_largest[EPI == I8_OUT ? 1 : BM];
   lds_byte_t* const s0 = (lds_byte_t*)stage0;
   lds_byte_t* const s1 = (lds_byte_t*)stage1;
@@ -324,11 +342,29 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
       __hip_atomic_fetch_max(&p.largest[t.row0 + threadIdx.x], row_largest[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   };
+  // The scales come by direct loads, behind the first operand tiles: nothing waits for them before the K loop's own waits do.  (One
+  // wave per 64 rows, one per 64 columns.)  The token of a gathered row is fetched a tile ahead.
+  auto scale_row = [&](const RowTile& t) { return t.row0 + min((int)threadIdx.x & (BM - 1), t.rows_valid - 1); };
+  auto fetch_scales = [&](const RowTile& t, int src) {
+    const float* from;
+    unsigned to;
+    if (wave < 4) {
+      from = p.xscale + (GATHER ? src / p.gk : scale_row(t));
+      to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) float*)row_scale + wave * 256;
+    } else {
+      const int c = threadIdx.x - BM;                    // column of the tile
+      const int col = GATE ? (c >> 6) * 32 + (c & 31) : c;
+      from = p.wscale + (size_t)t.e * (GATE ? 2 * NC : NC) + t.n0 + min(col, t.cols_valid - 1) + (GATE && (c >> 5) & 1 ? NC : 0);
+      to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) float*)col_scale + (wave - 4) * 256;
+    }
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
+  };
   unsigned idx = blockIdx.x;
   TileId id;
   if (!find_tile(seq, &idx, G, &id)) return;
   RowTile t = fetch_tile(id), before = t;
   before.rows_valid = 0;
+  int src = GATHER ? p.gsrc[scale_row(t)] : 0;
   Issue issue = make_issue(t);
   dma_prefetch3(s0, s1, s2, issue);
   for (;;) {
@@ -343,25 +379,27 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
     dma_pipeline_cont<false, false>(
         s0, s1, s2, s3, acc, issue, K / DK, next, wm, cb0,
         [&]() {
-          if (threadIdx.x < BM) {
+          fetch_scales(t, src);
+          if (EPI != I8_OUT && threadIdx.x < BM) {
             flush(before);
-            if (EPI != I8_OUT) row_largest[threadIdx.x] = 0;
-            const int row = t.row0 + min((int)threadIdx.x, t.rows_valid - 1);
-            row_scale[threadIdx.x] = p.xscale[GATHER ? p.gsrc[row] / p.gk : row];
+            row_largest[threadIdx.x] = 0;
           }
+          if (GATHER) src = p.gsrc[scale_row(tn)];
         },
         [&](Issue& nx) {
           if constexpr (!GATHER) nx = make_issue(tn);
         });
     lds_byte_t* const patch = s3 + wave * 4096;
-    const bool full = t.rows_valid == BM && t.cols_valid == TN;
+    const bool plain = t.rows_valid == BM && t.cols_valid == TN && !p.bias;      // the usual tile: no predicates, no bias
     if constexpr (EPI == I8_OUT) {
-      if (full) i8_rounds<EPI, T, FLEXMOE_RELU, true>(patch, acc, p, t, wave, row_scale, row_largest);
-      else i8_rounds<EPI, T, FLEXMOE_RELU, false>(patch, acc, p, t, wave, row_scale, row_largest);
+      if (plain) i8_rounds<EPI, T, FLEXMOE_RELU, true, false>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
+      else if (p.bias) i8_rounds<EPI, T, FLEXMOE_RELU, false, true>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
+      else i8_rounds<EPI, T, FLEXMOE_RELU, false, false>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
     } else {
       FLEXMOE_I8_BY_ACT(p.act, {
-        if (full) i8_rounds<EPI, T, ACT, true>(patch, acc, p, t, wave, row_scale, row_largest);
-        else i8_rounds<EPI, T, ACT, false>(patch, acc, p, t, wave, row_scale, row_largest);
+        if (plain) i8_rounds<EPI, T, ACT, true, false>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
+        else if (p.bias) i8_rounds<EPI, T, ACT, false, true>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
+        else i8_rounds<EPI, T, ACT, false, false>(patch, acc, p, t, wave, row_scale, col_scale, row_largest);
       })
     }
     before = t;
