@@ -283,6 +283,7 @@ void launch_rows_plan(const FfnArgs& a, void* ws, hipStream_t s) {
 RowsKernels rows_kernels(const FfnArgs& a, void* ws) {
   RowsKernels r;
   r.small = small_plan_ws(a, ws, &r.small_partial);
+  r.small_slots = r.small.bm ? (int)std::max(small_slots(a.A, a.E, r.small.bm, a.d, a.f), small_slots(a.A, a.E, r.small.bm, a.f, a.d)) : 0;
   r.row_tab = rows_tab_ws(a, ws);
   return r;
 }
@@ -426,18 +427,13 @@ void launch_bwd_plan(const FfnArgs& a, int fh, void* ws, hipStream_t s) {
                      geo[0], geo[1], rows_tab_ws(a, ws), small_plan_ws(a, ws));
 }
 
-// Sums of the partial tiles of `n` products (their [M, NC] have the same number of elements).
+// Sums of the partial tiles of `n` products.
 static void launch_wgrad_reduce(const FfnArgs& a, const WgradDmaArgs* g, int n, hipStream_t s) {
   if (!g->seg_tiles) return;
-  if (n == 2 && (size_t)g[0].M * g[0].NC != (size_t)g[1].M * g[1].NC) {
-    launch_wgrad_reduce(a, &g[0], 1, s);
-    launch_wgrad_reduce(a, &g[1], 1, s);
-    return;
-  }
-  const size_t elems = (size_t)g->M * g->NC;
+  const size_t elems = std::max((size_t)g[0].M * g[0].NC, (size_t)g[n - 1].M * g[n - 1].NC);
   const int blocks = (int)std::min<size_t>((elems / 4 + kGemmThreads - 1) / kGemmThreads, 2048);
-  const WgradReduceArgs r{(const int4*)g->plan.table, {{g[0].partial, g[0].dw}, {g[n - 1].partial, g[n - 1].dw}}};
-  hipLaunchKernelGGL(wgrad_reduce_kernel, dim3(blocks, a.E, n), dim3(kGemmThreads), 0, s, r, elems);
+  const WgradReduceArgs r{(const int4*)g->plan.table, {{g[0].partial, g[0].dw, (size_t)g[0].M * g[0].NC}, {g[n - 1].partial, g[n - 1].dw, (size_t)g[n - 1].M * g[n - 1].NC}}};
+  hipLaunchKernelGGL(wgrad_reduce_kernel, dim3(blocks, a.E, n), dim3(kGemmThreads), 0, s, r);
 }
 
 static bool overlap(const void* p, const void* q, size_t bytes_p, size_t bytes_q) {

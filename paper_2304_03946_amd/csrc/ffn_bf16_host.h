@@ -10,6 +10,7 @@ namespace flexmoe {
 struct RowsKernels {
   SmallPlan small;
   float* small_partial;
+  int small_slots;               // of BM x 128 sums
   i32x4* row_tab;
 };
 RowsKernels rows_kernels(const FfnArgs& a, void* ws);

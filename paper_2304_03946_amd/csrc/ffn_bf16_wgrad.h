@@ -677,11 +677,13 @@ struct WgradReduceArgs {
   struct {
     const float* partial;
     bf16_t* dw;
+    size_t elems;                // of the product's [M, NC]
   } p[2];
 };
-__global__ __launch_bounds__(kGemmThreads) void wgrad_reduce_kernel(const WgradReduceArgs a, size_t elems) {
+__global__ __launch_bounds__(kGemmThreads) void wgrad_reduce_kernel(const WgradReduceArgs a) {
   const int4 t = a.table[blockIdx.y];           // {expert, segments, first slot}
   if (t.y <= 1) return;
+  const size_t elems = a.p[blockIdx.z].elems;
   const size_t n4 = elems / 4;
   const float4* p = (const float4*)(a.p[blockIdx.z].partial + (size_t)t.z * elems);
   uint2* out = (uint2*)(a.p[blockIdx.z].dw + (size_t)t.x * elems);

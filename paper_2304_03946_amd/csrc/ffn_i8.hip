@@ -439,11 +439,12 @@ template <int RB, int EPI, typename T> struct I8SmallPol {
     return v;
   }
   template <int ACT>
-  __device__ __forceinline__ void out(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
+  __device__ __forceinline__ void out(const i32x4 (&acc1)[1][RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
                                       const I8Ahead<RB>& v) const {
     constexpr bool GATE = EPI == I8_GATE;
     const int NC = p.NC;
     const float(&cs)[2][4] = v.cs, (&b)[2][4] = v.b;
+    const i32x4(&acc)[RB][2] = acc1[0];
     bool ok[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) ok[j] = n0 + (GATE ? wave * 16 : wave * 32 + j * 16) + fg * 4 < NC;
@@ -479,7 +480,7 @@ template <int RB, int EPI, typename T> struct I8SmallPol {
       }
     }
   }
-  __device__ __forceinline__ void epilogue(const i32x4 (&acc)[RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
+  __device__ __forceinline__ void epilogue(const i32x4 (&acc)[1][RB][2], const SmallTile& t, const int (&orow)[RB], int n0, int wave, int fr, int fg,
                                            const I8Ahead<RB>& v) const {
     if constexpr (EPI == I8_OUT) out<FLEXMOE_RELU>(acc, t, orow, n0, wave, fr, fg, v);
     else FLEXMOE_I8_BY_ACT(p.act, out<ACT>(acc, t, orow, n0, wave, fr, fg, v))
@@ -490,7 +491,7 @@ template <int BM> constexpr int i8_cols() { return BM == 64 ? 128 : 64; }
 template <int BM, int EPI, typename T> __global__ __launch_bounds__(kSmallThreads, 2) void i8_small(const SmallCore c, const I8Args p) {
   __shared__ __align__(1024) unsigned char smem[CoreCfg<BM, i8_cols<BM>()>::kLds];
   const I8SmallPol<BM / 16, EPI, T> pol{p};
-  small_core<BM, i8_cols<BM>(), true, EPI == I8_GATE, i32x4>(c, pol, smem, blockIdx.x, gridDim.x);
+  small_core<BM, i8_cols<BM>(), true, EPI == I8_GATE ? GATE_MIXED : GATE_NONE, i32x4>(c, pol, smem, blockIdx.x, gridDim.x);
 }
 
 // ---- plan: what the products look up, the rows' integers and the zeros of `largest`, in one launch ----------------------
@@ -579,7 +580,7 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
   if (bm) {
     const int wcols = GATE ? 2 * p.NC : p.NC;
     const int cols = bm == 64 ? i8_cols<64>() : i8_cols<16>();
-    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters};
+    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters, kSmallSlots};
     const long long most = ((long long)a.A / bm + a.E) * c.col_tiles * kSmallSplitMax;
     const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
     if (bm == 16) hipLaunchKernelGGL((i8_small<16, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);

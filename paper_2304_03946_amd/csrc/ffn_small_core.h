@@ -13,8 +13,11 @@ namespace flexmoe {
 //  * V4, the type of four sums: f32x4 (bf16 operands) or i32x4 (8-bit integers, 128 of them to a stage: one instruction takes the
 //    same 16 bytes per lane in either case).  K and the operands' offsets count two-byte units, so 8-bit operands pass K / 2.
 //    Sums of integers are exact: segments change nothing, and a row's bits do not depend on the other rows.
-//  * GATED: the tile's 128 weight columns are 64 columns of the first half (gate) and the same 64 of the second (up), 16 and 16 in
-//    turn, so that a wave holds both values of an output in the same lane: acc[i][0] and acc[i][1].
+//  * GATE: a wave holds the gate's and up's values of an output in the same lane.  GATE_MIXED: the tile's weight columns are half from the
+//    first half (gate), half from the second (up), 16 and 16 in turn: acc[0][i][0] and acc[0][i][1].  GATE_TURNS (not WT): 128 columns of
+//    each half, whose stages alternate: acc[0][i][j] and acc[1][i][j].  That makes pieces of 256 bytes of a weight row instead of 128 -- a
+//    decode step of 16 tokens (d 1024, f 4096, 21 experts) reads them at 4.9 TB/s instead of 4.2 -- but half as many tiles of twice the
+//    latency: a step of 4 tokens (d 96, f 256) is 6 % slower.
 //  * COLS: a tile is 128 columns and a stage 128 bytes of k, or (WT) 64 columns and 256 bytes: HBM serves pieces of 256 bytes better than
 //    lines 4 KB and more apart.  With 64 columns two waves share an output block, each with half of a stage's k, and add their sums at
 //    the end.
@@ -30,6 +33,7 @@ struct SmallCore {
   const int32_t* inmap;          // position in expert order -> row of `in` (rowmap, or gathered rows)
   float* partial;
   int* counters;
+  int slots;                     // partial tiles of BM x 128 there is room for
 };
 struct SmallTile {
   int first, rows, e, ct;        // position in rowmap, rows, expert, column tile
@@ -44,16 +48,26 @@ template <int BM, int COLS> struct CoreCfg {
   static constexpr int kKUnits = kKBytes / 2;            // two-byte units of k in a stage
   static_assert(kALoads >= 1 && S >= 3 && S <= 4, "small_wait");
 };
-// segments of a contraction: small_segments, in stages of 128 bytes of k
-__host__ __device__ inline int core_segments(int tiles, int k_units) { return small_segments(tiles, (k_units + SK - 1) / SK); }
+// Segments of a contraction: those of small_segments in stages of 128 bytes of k, and three instead of two where three still fit the two
+// workgroups per compute unit (168 tiles of a decode step's second product: 504 workgroups instead of 336, 43.5 -> 39.6 us; with few tiles
+// a further segment costs more than it gains: 55 tiles of 12 stages, +5 %).  `tiles` counts partial tiles, of which there is room for `slots`.
+__device__ __forceinline__ int core_segments(int tiles, int k_units, int slots) {
+  const int k_tiles = (k_units + SK - 1) / SK;
+  int s = small_segments(tiles, k_tiles);
+  if (s == 2 && tiles > kSmallSplitTarget / 4 && tiles * 3 <= kSmallSplitTarget && k_tiles >= 3 * kSmallSplitKTiles) s = 3;
+  while (s > 1 && (long long)tiles * s > slots) --s;
+  return s;
+}
+enum { GATE_NONE = 0, GATE_MIXED = 1, GATE_TURNS = 2 };
 
-template <int BM, int COLS, bool WT, bool GATED, typename V4, typename Pol>
+template <int BM, int COLS, bool WT, int GATE, typename V4, typename Pol>
 __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, unsigned char* smem, unsigned block, unsigned blocks) {
   typedef CoreCfg<BM, COLS> C;
-  static_assert(COLS == 128 || (COLS == 64 && WT), "tile");
+  static_assert((COLS == 128 || (COLS == 64 && WT)) && !(WT && GATE == GATE_TURNS), "tile");
   constexpr int S = C::S, RB = BM / 16, NB2 = 2;         // 16-row and 16-column blocks of a wave
   constexpr int kPer = C::kKBytes / 16, kRows = 64 / kPer;      // 16-byte chunks of a row in a stage, rows of a direct load
   constexpr int kKWaves = COLS == 64 ? 2 : 1;            // waves that share an output block
+  constexpr int H = GATE == GATE_TURNS ? 2 : 1;                // stages per k and accumulators: the two halves in turn
   constexpr int kActive = kSmallThreads / kKWaves;       // threads with outputs
   lds_byte_t* const sm = (lds_byte_t*)smem;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)sm);
@@ -66,7 +80,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
   const int rows_act = tab[0][0];
   const int k_tiles = (K + C::kKUnits - 1) / C::kKUnits;
   const int tiles = rows_act * p.col_tiles;
-  const int nseg = core_segments(tiles, K);
+  const int nseg = core_segments(tiles * H, K, p.slots);
   // without segments: the XCD-aware patch order; with them: tile-major, a tile's segments side by side
   const unsigned total = nseg > 1 ? (unsigned)(tiles * nseg) : patched_grid(rows_act, p.col_tiles);
 
@@ -92,9 +106,10 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
     }
     const i32x4 d = tab[1 + rt];
     const SmallTile t{d[0], d[1], d[2], ct};
-    // first column of the tile, and columns there are (GATED: of either half)
-    const int n0 = ct * (GATED ? COLS / 2 : COLS), cols = min(GATED ? COLS / 2 : COLS, (GATED ? half : NC) - n0);
-    const int kt0 = (int)((long long)k_tiles * seg / nseg), kt1 = (int)((long long)k_tiles * (seg + 1) / nseg);
+    // first column of the tile, and columns there are (GATE: of either half)
+    constexpr int kCols = GATE == GATE_MIXED ? COLS / 2 : COLS;
+    const int n0 = ct * kCols, cols = min(kCols, (GATE ? half : NC) - n0);
+    const int kt0 = H * (int)((long long)k_tiles * seg / nseg), kt1 = H * (int)((long long)k_tiles * (seg + 1) / nseg);      // stages
     const bf16_t* w_e = p.w + (size_t)t.e * K * NC + (WT ? (size_t)n0 * K : (size_t)n0);
 
     // rows of the wave's loads (rows past the tile repeat its last row) and of its outputs
@@ -112,7 +127,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
     const auto ahead = pol.before(t, p.inmap, n0, cw, fr, fg);
     uint32_t woff[C::kWLoads];
     int wk[C::kWLoads];                                  // k (in the stage) of the lane's first element
-    size_t wbase[C::kWLoads];                            // (uniform) where the load's rows start behind w_e: GATED && WT, the up half
+    size_t wbase[C::kWLoads];                            // (uniform) where the load's rows start behind w_e: GATE_MIXED && WT, the up half
 #pragma unroll
     for (int q = 0; q < C::kWLoads; ++q) {
       const int i = wave * C::kWLoads + q;
@@ -120,7 +135,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       if (WT) {
         int row = i * kRows + lane / kPer;
         wk[q] = ((lane % kPer) ^ (row & (kPer - 1))) * 8;
-        if (GATED) {
+        if (GATE) {
           row = (row >> 5) * 16 + (row & 15);
           if (((i * kRows) >> 4) & 1) wbase[q] = (size_t)half * K;
         }
@@ -129,7 +144,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
         const int kr = i * 4 + (lane >> 4);
         wk[q] = kr;
         int c = (lane & 15) ^ ((kr & 3) << 2) ^ ((kr & 8) >> 2), up = 0;
-        if (GATED) {
+        if (GATE == GATE_MIXED) {
           up = (c >> 1) & 1 ? half : 0;
           c = (c >> 2) * 2 + (c & 1);
         }
@@ -138,8 +153,8 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
     }
     auto issue = [&](int kt) {
       const unsigned st = lds0 + (unsigned)((kt - kt0) % S) * C::kStage;
-      const int k0 = kt * C::kKUnits;
-      const bf16_t* wb = w_e + (WT ? (size_t)k0 : (size_t)k0 * NC);
+      const int k0 = kt / H * C::kKUnits;
+      const bf16_t* wb = w_e + (WT ? (size_t)k0 : (size_t)k0 * NC + (H == 2 && (kt & 1) ? half : 0));
       if (k0 + C::kKUnits <= K) {
 #pragma unroll
         for (int q = 0; q < C::kALoads; ++q) small_load_at(aptr[q] + k0, st + (wave * C::kALoads + q) * 1024);
@@ -156,17 +171,19 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       }
     };
 
-    V4 acc[RB][NB2];
+    V4 acc[H][RB][NB2];
 #pragma unroll
-    for (int i = 0; i < RB; ++i)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int j = 0; j < NB2; ++j) acc[i][j] = V4{0, 0, 0, 0};
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB2; ++j) acc[h][i][j] = V4{0, 0, 0, 0};
 
     __syncthreads();                                     // the previous tile's epilogue has left the stages
 #pragma unroll
     for (int q = 0; q < S - 1; ++q)
       if (kt0 + q < kt1) issue(kt0 + q);
-    for (int kt = kt0; kt < kt1; ++kt) {
+    auto step = [&](int kt, V4(&acc)[RB][NB2]) {
       small_wait<C::kLoads>(min(S - 2, kt1 - 1 - kt));
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
       __builtin_amdgcn_s_barrier();
@@ -196,7 +213,10 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
 #pragma unroll
           for (int j = 0; j < NB2; ++j) acc[i][j] = mma_16x16(w[j], a[i], acc[i][j]);
       }
-    }
+    };
+    for (int kt = kt0; kt < kt1; kt += H)
+#pragma unroll
+      for (int h = 0; h < H; ++h) step(kt + h, acc[h]);
     __syncthreads();                                     // every wave has left the last stage
     if (kKWaves == 2) {
       typedef __attribute__((address_space(3))) V4* Ptr;
@@ -205,14 +225,14 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int j = 0; j < NB2; ++j) at[(i * NB2 + j) * kActive] = acc[i][j];
+          for (int j = 0; j < NB2; ++j) at[(i * NB2 + j) * kActive] = acc[0][i][j];
       }
       __syncthreads();
       if (kw == 0) {
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int j = 0; j < NB2; ++j) acc[i][j] += at[(i * NB2 + j) * kActive];
+          for (int j = 0; j < NB2; ++j) acc[0][i][j] += at[(i * NB2 + j) * kActive];
       }
     }
 
@@ -221,14 +241,16 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       const int tile = rt * p.col_tiles + ct;
       typedef unsigned long long u64;
       typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      u64* part = (u64*)(p.partial + (size_t)tile * nseg * (BM * COLS));
+      u64* part = (u64*)(p.partial + (size_t)tile * nseg * (H * BM * COLS));
       if (kw == 0) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
           for (int j = 0; j < NB2; ++j) {
-            u64* dst = part + (size_t)seg * (BM * COLS / 2) + (i * NB2 + j) * (2 * kActive) + threadIdx.x;
-            const u32x4 bits = __builtin_bit_cast(u32x4, acc[i][j]);
+            u64* dst = part + (size_t)seg * (H * BM * COLS / 2) + ((h * RB + i) * NB2 + j) * (2 * kActive) + threadIdx.x;
+            const u32x4 bits = __builtin_bit_cast(u32x4, acc[h][i][j]);
             __hip_atomic_store(dst, (u64)bits[0] | (u64)bits[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             __hip_atomic_store(dst + kActive, (u64)bits[2] | (u64)bits[3] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           }
@@ -246,23 +268,25 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       if (threadIdx.x == 0) p.counters[tile] = 0;        // as the plan left it: the call's next product counts there too
       if (kw == 0) {
 #pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
           for (int j = 0; j < NB2; ++j) {
             V4 s = V4{0, 0, 0, 0};
             for (int g = 0; g < nseg; ++g) {
-              u64* from = part + (size_t)g * (BM * COLS / 2) + (i * NB2 + j) * (2 * kActive) + threadIdx.x;
+              u64* from = part + (size_t)g * (H * BM * COLS / 2) + ((h * RB + i) * NB2 + j) * (2 * kActive) + threadIdx.x;
               const u64 lo = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
               const u64 hi = __hip_atomic_load(from + kActive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
               s += __builtin_bit_cast(V4, u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)});
             }
-            acc[i][j] = s;
+            acc[h][i][j] = s;
           }
       }
       __syncthreads();                                   // the flag has been read
     }
     // lane: row 16 i + fr of the tile (bucket row orow[i], there if 16 i + fr < rows), four columns from 4 fg on of 16-column block
-    // 2 cw + j (GATED: j = 0 gate, 1 up, of columns n0 + 16 cw + 4 fg ..)
+    // 2 cw + j (GATE_MIXED: j = 0 gate, 1 up, of columns n0 + 16 cw + 4 fg ..)
     if (kw == 0) pol.epilogue(acc, t, orow, n0, cw, fr, fg, ahead);
   }
 }
