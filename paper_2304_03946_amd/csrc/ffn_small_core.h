@@ -267,21 +267,33 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
       if (!last) continue;
       if (threadIdx.x == 0) p.counters[tile] = 0;        // as the plan left it: the call's next product counts there too
       if (kw == 0) {
+        // as many segments at a time as 128 registers hold: each is a trip past the L2
+        constexpr int kSums = H * RB * NB2, kBatch = 32 / kSums;
+        V4 s[kSums];
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+        for (int x = 0; x < kSums; ++x) s[x] = V4{0, 0, 0, 0};
+        for (int g0 = 0; g0 < nseg; g0 += kBatch) {
+          u64 lo[kBatch][kSums], hi[kBatch][kSums];
 #pragma unroll
-        for (int i = 0; i < RB; ++i)
+          for (int b = 0; b < kBatch; ++b)
+            if (g0 + b < nseg) {
 #pragma unroll
-          for (int j = 0; j < NB2; ++j) {
-            V4 s = V4{0, 0, 0, 0};
-            for (int g = 0; g < nseg; ++g) {
-              u64* from = part + (size_t)g * (H * BM * COLS / 2) + ((h * RB + i) * NB2 + j) * (2 * kActive) + threadIdx.x;
-              const u64 lo = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              const u64 hi = __hip_atomic_load(from + kActive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              s += __builtin_bit_cast(V4, u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)});
+              for (int x = 0; x < kSums; ++x) {
+                u64* from = part + (size_t)(g0 + b) * (H * BM * COLS / 2) + x * (2 * kActive) + threadIdx.x;
+                lo[b][x] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                hi[b][x] = __hip_atomic_load(from + kActive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+              }
             }
-            acc[h][i][j] = s;
-          }
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b)
+            if (g0 + b < nseg) {
+#pragma unroll
+              for (int x = 0; x < kSums; ++x)
+                s[x] += __builtin_bit_cast(V4, u32x4{(uint32_t)lo[b][x], (uint32_t)(lo[b][x] >> 32), (uint32_t)hi[b][x], (uint32_t)(hi[b][x] >> 32)});
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kSums; ++x) acc[x / (RB * NB2)][x / NB2 % RB][x % NB2] = s[x];
       }
       __syncthreads();                                   // the flag has been read
     }
