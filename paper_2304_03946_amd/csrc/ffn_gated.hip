@@ -605,7 +605,7 @@ static hipError_t launch_gated_out(const FfnArgs& a, const void* h, const void* 
   if (!rk.small.bm) return launch_rows_plain(a, h, w2, b2, f, yp, ws, s);
   const GatedArgs p{(const bf16_t*)h, (const bf16_t*)w2, (const bf16_t*)b2, a.voff, a.owner, a.V, f, a.d, 0, 0, nullptr, (bf16_t*)yp, nullptr, 0};
   const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, f, a.d, (a.d + SN - 1) / SN, rk.small.rowmap, rk.small_partial, rk.small.counters,
-                    rk.small_slots};
+                    rk.small_slots, a.A};
   const dim3 grid(small_grid(a, rk.small.bm, c.col_tiles));
   if (rk.small.bm == 32) hipLaunchKernelGGL(gated_out_small_bf16<32>, grid, dim3(kSmallThreads), 0, s, c, p);
   else hipLaunchKernelGGL(gated_out_small_bf16<64>, grid, dim3(kSmallThreads), 0, s, c, p);
@@ -625,7 +625,7 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
     const bool turns = FWD && (long long)std::min(a.A, a.E) * ((f + SN - 1) / SN) >= kSmallSplitTarget;
     const int cols = FWD && !turns ? SN / 2 : SN;
     const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, K, FWD ? 2 * f : f, (f + cols - 1) / cols, rk.small.rowmap, rk.small_partial,
-                      rk.small.counters, rk.small_slots};
+                      rk.small.counters, rk.small_slots, a.A};
     const dim3 grid(small_grid(a, rk.small.bm, c.col_tiles));
     constexpr int kGate = FWD ? GATE_MIXED : GATE_NONE;
     if constexpr (FWD) {

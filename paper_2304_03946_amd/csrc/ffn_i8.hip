@@ -580,7 +580,7 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
   if (bm) {
     const int wcols = GATE ? 2 * p.NC : p.NC;
     const int cols = bm == 64 ? i8_cols<64>() : i8_cols<16>();
-    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters, kSmallSlots};
+    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters, kSmallSlots, a.A};
     const long long most = ((long long)a.A / bm + a.E) * c.col_tiles * kSmallSplitMax;
     const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
     if (bm == 16) hipLaunchKernelGGL((i8_small<16, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);

@@ -34,6 +34,7 @@ struct SmallCore {
   float* partial;
   int* counters;
   int slots;                     // partial tiles of BM x 128 there is room for
+  int rows;                      // of all buckets
 };
 struct SmallTile {
   int first, rows, e, ct;        // position in rowmap, rows, expert, column tile
@@ -48,13 +49,17 @@ template <int BM, int COLS> struct CoreCfg {
   static constexpr int kKUnits = kKBytes / 2;            // two-byte units of k in a stage
   static_assert(kALoads >= 1 && S >= 3 && S <= 4, "small_wait");
 };
-// Segments of a contraction: those of small_segments in stages of 128 bytes of k, and three instead of two where three still fit the two
-// workgroups per compute unit (168 tiles of a decode step's second product: 504 workgroups instead of 336, 43.5 -> 39.6 us; with few tiles
-// a further segment costs more than it gains: 55 tiles of 12 stages, +5 %).  `tiles` counts partial tiles, of which there is room for `slots`.
-__device__ __forceinline__ int core_segments(int tiles, int k_units, int slots) {
-  const int k_tiles = (k_units + SK - 1) / SK;
-  int s = small_segments(tiles, k_tiles);
-  if (s == 2 && tiles > kSmallSplitTarget / 4 && tiles * 3 <= kSmallSplitTarget && k_tiles >= 3 * kSmallSplitKTiles) s = 3;
+// Segments of a contraction of k_stages stages: a power of two as long as two workgroups per compute unit take them all (and three where
+// that is what fits: 168 tiles of a decode step's second product, 504 workgroups instead of 336, 43.5 -> 39.6 us), each at least
+// four stages long, eight where tiles have more than 16 rows on average, whose partial tiles are the more traffic.  In us, at least four and at
+// least eight: 522 rows of 7 experts (d 408, f 2080) 35.0, 28.6; 4503 of 12 (training) 145.7, 136.4; 600 8-bit rows of 8 experts
+// 21.7, 20.0; few rows per tile: 5 rows of one expert (d 1664, f 1608) 21.6, 26.2; 8 8-bit rows (1696 x 1808) 16.9, 18.2.
+// `tiles` counts partial tiles, of which there is room for `slots`.
+__device__ __forceinline__ int core_segments(int tiles, int k_stages, int row_tiles, int rows, int slots) {
+  const int least = rows > 16 * row_tiles ? 2 * kSmallSplitKTiles : kSmallSplitKTiles;
+  int s = 1;
+  while (s < kSmallSplitMax && tiles * s * 2 <= kSmallSplitTarget && k_stages >= 2 * s * least) s *= 2;
+  if (s == 2 && tiles > kSmallSplitTarget / 4 && tiles * 3 <= kSmallSplitTarget && k_stages >= 3 * least) s = 3;
   while (s > 1 && (long long)tiles * s > slots) --s;
   return s;
 }
@@ -80,7 +85,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
   const int rows_act = tab[0][0];
   const int k_tiles = (K + C::kKUnits - 1) / C::kKUnits;
   const int tiles = rows_act * p.col_tiles;
-  const int nseg = core_segments(tiles * H, K, p.slots);
+  const int nseg = core_segments(tiles * H, k_tiles, rows_act, p.rows, p.slots);
   // without segments: the XCD-aware patch order; with them: tile-major, a tile's segments side by side
   const unsigned total = nseg > 1 ? (unsigned)(tiles * nseg) : patched_grid(rows_act, p.col_tiles);
 
@@ -249,6 +254,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
         for (int i = 0; i < RB; ++i)
 #pragma unroll
           for (int j = 0; j < NB2; ++j) {
+            if (i * 16 >= t.rows) continue;              // (uniform: blocks without rows do not travel)
             u64* dst = part + (size_t)seg * (H * BM * COLS / 2) + ((h * RB + i) * NB2 + j) * (2 * kActive) + threadIdx.x;
             const u32x4 bits = __builtin_bit_cast(u32x4, acc[h][i][j]);
             __hip_atomic_store(dst, (u64)bits[0] | (u64)bits[1] << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -279,6 +285,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
             if (g0 + b < nseg) {
 #pragma unroll
               for (int x = 0; x < kSums; ++x) {
+                if (x / NB2 % RB * 16 >= t.rows) continue;
                 u64* from = part + (size_t)(g0 + b) * (H * BM * COLS / 2) + x * (2 * kActive) + threadIdx.x;
                 lo[b][x] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 hi[b][x] = __hip_atomic_load(from + kActive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -289,7 +296,7 @@ __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, u
             if (g0 + b < nseg) {
 #pragma unroll
               for (int x = 0; x < kSums; ++x)
-                s[x] += __builtin_bit_cast(V4, u32x4{(uint32_t)lo[b][x], (uint32_t)(lo[b][x] >> 32), (uint32_t)hi[b][x], (uint32_t)(hi[b][x] >> 32)});
+                if (x / NB2 % RB * 16 < t.rows) s[x] += __builtin_bit_cast(V4, u32x4{(uint32_t)lo[b][x], (uint32_t)(lo[b][x] >> 32), (uint32_t)hi[b][x], (uint32_t)(hi[b][x] >> 32)});
             }
         }
 #pragma unroll
