@@ -11,8 +11,9 @@
 //  * a tile of the first product holds a column of G and the same column of U in the same lane: its weight columns are taken from the two
 //    halves of W1 in turn, 32 and 32.  Only the addresses of the weights' loads know about it.
 //  * G, U and H leave through a wave-private LDS patch as bf16 (half of what fp32 patches move): 16 bytes per lane, 64 per row.
-//  * three sets of kernels, chosen as for an ungated layer with 2 f columns: rows of 256 x 256 tiles with direct-to-LDS loads where K is a
-//    multiple of 128, register-staged ones for other K, and 32- or 64-row tiles for few rows (small_core; there the halves take turns).
+//  * two sets of kernels, chosen as for an ungated layer with 2 f columns: 256 x 256 tiles with direct-to-LDS loads for any K (a contraction
+//    that is no multiple of 128 ends in zeros, ffn_ragged_src.h; Y's product is here as well for such f), and 32- or 64-row tiles for few
+//    rows (small_core).
 // Rounding: H is made of the fp32 sums and rounded once.  What is kept of G and U for the backward pass are 16-bit words with two mantissa
 // bits more than bf16 has (keep4): as bf16 they put as much error into the gradients as the rounding of dHpre that cannot be
 // avoided (rel. error of dW1 and dX, 64-bit formula: 0.0030 with bf16 words, 0.0024 with these, 0.0017 is the rounding of the output alone).
@@ -26,6 +27,7 @@
 #include "ffn_bf16_dma.h"
 #include "ffn_bf16_persist.h"
 #include "ffn_bf16_small.h"
+#include "ffn_ragged_src.h"
 #include "ffn_small_core.h"
 
 namespace flexmoe {
@@ -81,10 +83,8 @@ __device__ __forceinline__ void kept4(uint2 w, float* v) {
 struct GatedArgs {
   const bf16_t* in;              // fwd: Xp, dH: dYp
   const bf16_t* w;               // fwd: W1 [E, d, 2 f], dH: W2 [E, f, d]
-  const bf16_t* bias;            // [E, 2 f] or null (fwd)
-  const int32_t* voff;
-  const int32_t* owner;
-  int V, K, f, row_tiles_max, col_tiles;
+  const bf16_t* bias;            // [E, 2 f] or null (fwd), [E, f] or null (plain)
+  int K, f, col_tiles;           // f: columns of H, or of the plain product's output
   const bf16_t* hpre_in;         // dH: Hpre [A, 2 f], kept words
   bf16_t* out0;                  // fwd: Hpre (kept words) or null, dH: dHpre [A, 2 f]
   bf16_t* out1;                  // fwd: H [A, f], dH: H or null (kept by the forward pass)
@@ -289,6 +289,48 @@ __device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaA
   }
 }
 
+// The plain product: 128 rows x 64 columns, 16 rows at a time as [16][64] bf16 (128-byte rows, chunk index XOR row / 2).
+template <bool FULL>
+__device__ __forceinline__ void gated_plain_rounds(lds_byte_t* patch, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wm, int c0) {
+  const int lane = opaque_tid() & 63;
+  const int r = lane & 15, g4 = lane >> 4;
+  const int NC = p.f;
+  float b[2][2][4] = {};
+  if (p.bias) {
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int sj = 0; sj < 2; ++sj) unpack4(*(const uint2*)(p.bias + (size_t)t.e * NC + min(c0 + 32 * jj + 16 * sj + 4 * g4, NC - 4)), b[jj][sj]);
+  }
+#pragma unroll
+  for (int round = 0; round < 2 * MB; ++round) {
+    const int i = round >> 1, sub = round & 1;
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int sj = 0; sj < 2; ++sj) {
+        const int e = 4 * (2 * sub + sj);
+        const f32x16& a = acc[i][jj];
+        const float* v = b[jj][sj];
+        *(__attribute__((address_space(3))) u32x2_t*)(patch + r * 128 + (((jj * 4 + sj * 2 + (g4 >> 1)) ^ (r >> 1)) << 4) + (g4 & 1) * 8) =
+            u32x2_t{pack_bf16x2(a[e] + v[0], a[e + 1] + v[1]), pack_bf16x2(a[e + 2] + v[2], a[e + 3] + v[3])};
+      }
+    asm volatile("" ::: "memory");                       // (a wave's LDS instructions execute in order)
+    u32x4_t v[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int row = k * 8 + (lane >> 3);
+      v[k] = *(const __attribute__((address_space(3))) u32x4_t*)(patch + row * 128 + (((lane & 7) ^ (row >> 1)) << 4));
+    }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int row = (wm + 2 * i) * 32 + sub * 16 + k * 8 + (lane >> 3), col = c0 + (lane & 7) * 8;
+      if (FULL || (row < t.rows_valid && col < NC)) *(u32x4_t*)(p.out0 + (size_t)(t.row0 + row) * NC + col) = v[k];
+    }
+  }
+}
+
 template <int EPI, int ACT>
 __device__ __forceinline__ void gated_epilogue(unsigned char* stage, const DmaAcc& acc, const GatedArgs& p, const RowTile& t, int wave) {
   const int wm = dma_wave_wm(wave), wn = wave & 1, hh = wave >> 2;
@@ -316,10 +358,10 @@ __device__ __forceinline__ void gated_epilogue(unsigned char* stage, const DmaAc
     default: { constexpr int ACT = FLEXMOE_SILU; call; break; }                    \
   }
 
-// The persistent kernel of either product (see rows_gemm_persist_bf16): 256 workgroups walk the tiles, the next tile's first loads go out
-// while the current K loop drains.  K a multiple of 128.  EPI_FWD1: a tile is 256 rows x 128 columns of H; EPI_DH, EPI_DHQ: 256 of dH.
-template <int EPI> __global__ __launch_bounds__(kDmaThreads) void gated_persist_bf16(const GatedArgs p, const i32x4* row_tab) {
-  constexpr bool FWD = EPI == EPI_FWD1;
+// The persistent kernel of these products (see rows_gemm_persist_bf16): 256 workgroups walk the tiles, the next tile's first loads go out
+// while the current K loop drains.  EPI_FWD1: a tile is 256 rows x 128 columns of H; EPI_DH, EPI_DHQ: 256 of dH; EPI_PLAIN: 256 of Y.
+template <int EPI, bool RAGGED> __global__ __launch_bounds__(kDmaThreads) void gated_persist_bf16(const GatedArgs p, const i32x4* row_tab) {
+  constexpr bool FWD = EPI == EPI_FWD1, STRIDED = FWD || EPI == EPI_PLAIN;
   __shared__ __align__(1024) unsigned char stage0[kDmaStageBytes];
   __shared__ __align__(1024) unsigned char stage1[kDmaStageBytes];
   __shared__ __align__(1024) unsigned char stage2[kDmaStageBytes];
@@ -328,12 +370,13 @@ template <int EPI> __global__ __launch_bounds__(kDmaThreads) void gated_persist_
   lds_byte_t* const s1 = (lds_byte_t*)stage1;
   lds_byte_t* const s2 = (lds_byte_t*)stage2;
   lds_byte_t* const s3 = (lds_byte_t*)stage3;
-  typedef typename std::conditional<FWD, DmaSrcGate, DmaSrc>::type WSrc;
-  typedef RowsIssueV<WSrc> Issue;
+  typedef typename std::conditional<FWD, RaggedCols<DmaSrcGate, RAGGED>,
+                                    typename std::conditional<STRIDED, RaggedCols<DmaSrcT, RAGGED>, RaggedRows<DmaSrc, RAGGED>>::type>::type WSrc;
+  typedef RaggedIssue<RaggedRows<DmaSrc, RAGGED>, WSrc> Issue;
 
   const RowTabPtr tab = (RowTabPtr)row_tab;
-  const int K = p.K, f = p.f;
-  const TileSeq seq = make_tile_seq(tab[0][0], p.col_tiles, false, K / DK);
+  const int K = p.K, f = p.f, KT = RAGGED ? ragged_k_tiles(K) : K / DK;
+  const TileSeq seq = make_tile_seq(tab[0][0], p.col_tiles, false, KT);
   const unsigned G = gridDim.x;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = dma_wave_wm(wave), cb0 = dma_wave_cb0(wave);
@@ -351,7 +394,9 @@ template <int EPI> __global__ __launch_bounds__(kDmaThreads) void gated_persist_
     Issue is;
     is.a_src.init(p.in + (size_t)t.row0 * K, K, t.rows_valid);
     if constexpr (FWD) is.w_src.init(p.w + (size_t)t.e * K * 2 * f + t.n0, f, t.cols_valid);
+    else if constexpr (STRIDED) is.w_src.init(p.w + (size_t)t.e * K * f + t.n0, f, t.cols_valid);
     else is.w_src.init(p.w + (size_t)t.e * K * f + (size_t)t.n0 * K, K, t.cols_valid);
+    is.a_src.K = is.w_src.K = K;
     is.k_next = 0;
     return is;
   };
@@ -369,123 +414,19 @@ template <int EPI> __global__ __launch_bounds__(kDmaThreads) void gated_persist_
     const bool has_next = find_tile(seq, &nidx, G, &nid);
     const RowTile tn = has_next ? fetch_tile(nid) : t;   // (none: this tile's first loads once more, waited for below and never used)
     Issue next;
-    dma_pipeline_cont<false, FWD>(s0, s1, s2, s3, acc, issue, K / DK, next, wm, cb0, []() {}, [&](Issue& nx) { nx = make_issue(tn); });
-    FLEXMOE_BY_ACT(p.act, (gated_epilogue<EPI, ACT>(stage3, acc, p, t, wave)))
+    dma_pipeline_cont<false, STRIDED>(s0, s1, s2, s3, acc, issue, KT, next, wm, cb0, []() {}, [&](Issue& nx) { nx = make_issue(tn); });
+    if constexpr (EPI == EPI_PLAIN) {
+      if (t.rows_valid == BM && t.cols_valid == BN) gated_plain_rounds<true>(s3 + wave * 4096, acc, p, t, wm, t.n0 + cb0 * 32);
+      else gated_plain_rounds<false>(s3 + wave * 4096, acc, p, t, wm, t.n0 + cb0 * 32);
+    } else {
+      FLEXMOE_BY_ACT(p.act, (gated_epilogue<EPI, ACT>(stage3, acc, p, t, wave)))
+    }
     if (!has_next) break;
     t = tn;
     issue = next;
     idx = nidx;
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): nothing may still be landing in LDS when the workgroup ends
-}
-
-// ---- register-staged kernels: any K that is a multiple of 8 -------------------------------------
-// KStridedSrc with the columns of DmaSrcGate.
-struct KStridedGateSrc : KStridedSrc {
-  __device__ __forceinline__ void init(int f, int cols_valid) {
-    const int c = threadIdx.x & 31, kc = threadIdx.x >> 5;
-    const int in_half = min((c >> 3) * 4 + (c & 3), cols_valid / 8 - 1);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      off[j] = (uint32_t)(kc * 8 + j) * 2u * (uint32_t)f + (uint32_t)in_half * 8u + ((c >> 2) & 1 ? (uint32_t)f : 0u);
-  }
-};
-// Lane L of a wave's 32 x 32 accumulator tile [i][j]: row L % 32, columns 8 (q / 4) + 4 (L / 32) + q % 4.  The outputs go out from there,
-// 8 bytes per lane: the products that come here are small or odd.
-template <int EPI, int ACT>
-__device__ __forceinline__ void gated_direct(const f32x16 (&acc)[MB][NB], const GatedArgs& p, const RowTile& t, int wm, int wn) {
-  const int lane = threadIdx.x & 63, f = p.f;
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int row = (wm + 2 * i) * 32 + (lane & 31);
-    if (row >= t.rows_valid) continue;
-    const size_t grow = t.row0 + row;
-#pragma unroll
-    for (int j = 0; j < NB; j += EPI == EPI_FWD1 ? 2 : 1)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int in_blk = 8 * g + 4 * (lane >> 5);
-        if (EPI == EPI_FWD1) {
-          const int col = t.n0 + ((wn * NB + j) >> 1) * 32 + in_blk;
-          if (col >= f) continue;
-          float z[4], u[4], h[4], b[4] = {}, bu[4] = {}, da;
-          if (p.bias) {
-            unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + col), b);
-            unpack4(*(const uint2*)(p.bias + (size_t)t.e * 2 * f + f + col), bu);
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            z[q] = acc[i][j][4 * g + q] + b[q];
-            u[q] = acc[i][j + 1 < NB ? j + 1 : j][4 * g + q] + bu[q];
-            gate_act<ACT>(z[q], &h[q], &da);
-            h[q] *= u[q];
-          }
-          if (p.out0) {
-            *(uint2*)(p.out0 + grow * 2 * f + col) = keep4(z);
-            *(uint2*)(p.out0 + grow * 2 * f + f + col) = keep4(u);
-          }
-          *(uint2*)(p.out1 + grow * f + col) = pack4(h[0], h[1], h[2], h[3]);
-        } else {
-          const int col = t.n0 + (wn * NB + j) * 32 + in_blk;
-          if (col >= f) continue;
-          float z[4], u[4], dg[4], du[4], h[4];
-          kept4(*(const uint2*)(p.hpre_in + grow * 2 * f + col), z);
-          kept4(*(const uint2*)(p.hpre_in + grow * 2 * f + f + col), u);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float dh = acc[i][j][4 * g + q];
-            float a, da;
-            gate_act<ACT>(z[q], &a, &da);
-            dg[q] = dh * u[q] * da;
-            du[q] = dh * a;
-            h[q] = a * u[q];
-          }
-          *(uint2*)(p.out0 + grow * 2 * f + col) = pack4(dg[0], dg[1], dg[2], dg[3]);
-          *(uint2*)(p.out0 + grow * 2 * f + f + col) = pack4(du[0], du[1], du[2], du[3]);
-          if (EPI == EPI_DH) *(uint2*)(p.out1 + grow * f + col) = pack4(h[0], h[1], h[2], h[3]);
-        }
-      }
-  }
-}
-template <int EPI> __global__ __launch_bounds__(kGemmThreads) void gated_staged_bf16(const GatedArgs p) {
-  constexpr bool FWD = EPI == EPI_FWD1;
-  __shared__ __align__(16) unsigned char smem_raw[kGemmLds];
-  bf16_t* smem = (bf16_t*)smem_raw;
-  __shared__ int s_tile[4];
-  RowTile t;
-  if (!lookup_row_tile(p.voff, p.owner, p.V, p.f, p.row_tiles_max, p.col_tiles, blockIdx.x, s_tile, &t)) return;
-  t.n0 = t.n0 / BN * (FWD ? GN : BN);
-  t.cols_valid = min(FWD ? GN : BN, p.f - t.n0);
-  const int K = p.K, f = p.f, KT = (K + BK - 1) / BK;
-  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
-  f32x16 acc[MB][NB];
-  zero_acc(acc);
-  KContigSrc a_src;
-  a_src.init(p.in + (size_t)t.row0 * K, K, t.rows_valid, K);
-  int ka = 0, kb = 0;
-  auto load_a = [&](uint4 (&ra)[8]) {
-    a_src.load(ra, ka);
-    ka += BK;
-  };
-  if constexpr (FWD) {
-    KStridedGateSrc w_src;
-    w_src.init(f, t.cols_valid);
-    const bf16_t* wp = p.w + (size_t)t.e * K * 2 * f + t.n0;
-    auto load_b = [&](uint4 (&rb)[8]) {
-      w_src.load(rb, wp + (size_t)kb * 2 * f, K - kb);
-      kb += BK;
-    };
-    run_pipeline<true>(smem, acc, KT, KContigSrc::store, KStridedSrc::store, load_a, load_b, wm, wn, 8);
-  } else {
-    KContigSrc w_src;
-    w_src.init(p.w + (size_t)t.e * K * f + (size_t)t.n0 * K, K, t.cols_valid, K);
-    auto load_b = [&](uint4 (&rb)[8]) {
-      w_src.load(rb, kb);
-      kb += BK;
-    };
-    run_pipeline<true>(smem, acc, KT, KContigSrc::store, KContigSrc::store, load_a, load_b, wm, wn, 8);
-  }
-  FLEXMOE_BY_ACT(p.act, (gated_direct<EPI, ACT>(acc, p, t, wm, wn)))
 }
 
 // ---- few rows ----------------------------------------------------------------------------------
@@ -599,11 +540,25 @@ template <int BM> __global__ __launch_bounds__(kSmallThreads, 2) void gated_out_
 static unsigned small_grid(const FfnArgs& a, int bm, int col_tiles) {
   return (unsigned)std::min<long long>(kSmallSplitTarget, ((long long)a.A / bm + a.E) * col_tiles * kSmallSplitMax);
 }
+template <int EPI> static void launch_persist(const FfnArgs& a, const GatedArgs& p, const RowsKernels& rk, hipStream_t s) {
+  const dim3 grid(std::min(patched_grid(a.A / BM + a.V, p.col_tiles), 256u));
+  if constexpr (EPI != EPI_PLAIN) {
+    if (p.K % (4 * DK) == 0) {
+      hipLaunchKernelGGL((gated_persist_bf16<EPI, false>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((gated_persist_bf16<EPI, true>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
+}
 static hipError_t launch_gated_out(const FfnArgs& a, const void* h, const void* w2, const void* b2, void* yp, void* ws, hipStream_t s) {
   const int f = a.f / 2;
   const RowsKernels rk = rows_kernels(a, ws);
-  if (!rk.small.bm) return launch_rows_plain(a, h, w2, b2, f, yp, ws, s);
-  const GatedArgs p{(const bf16_t*)h, (const bf16_t*)w2, (const bf16_t*)b2, a.voff, a.owner, a.V, f, a.d, 0, 0, nullptr, (bf16_t*)yp, nullptr, 0};
+  if (!rk.small.bm && f % 128 == 0) return launch_rows_plain(a, h, w2, b2, f, yp, ws, s);
+  const GatedArgs p{(const bf16_t*)h, (const bf16_t*)w2, (const bf16_t*)b2, f, a.d, (a.d + BN - 1) / BN, nullptr, (bf16_t*)yp, nullptr, 0};
+  if (!rk.small.bm) {
+    launch_persist<EPI_PLAIN>(a, p, rk, s);
+    return hipGetLastError();
+  }
   const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, f, a.d, (a.d + SN - 1) / SN, rk.small.rowmap, rk.small_partial, rk.small.counters,
                     rk.small_slots, a.A};
   const dim3 grid(small_grid(a, rk.small.bm, c.col_tiles));
@@ -618,8 +573,8 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
   constexpr bool FWD = EPI == EPI_FWD1;
   const int f = a.f / 2, K = a.d;
   const RowsKernels rk = rows_kernels(a, ws);
-  GatedArgs p{(const bf16_t*)in, (const bf16_t*)w, (const bf16_t*)bias, a.voff, a.owner, a.V, K, f, a.A / BM + a.V, 0,
-              (const bf16_t*)hpre_in, (bf16_t*)out0, (bf16_t*)out1, a.act};
+  const GatedArgs p{(const bf16_t*)in, (const bf16_t*)w, (const bf16_t*)bias, K, f, FWD ? (f + GN - 1) / GN : (f + BN - 1) / BN,
+                    (const bf16_t*)hpre_in, (bf16_t*)out0, (bf16_t*)out1, a.act};
   if (rk.small.bm) {
     // the halves in turn where that leaves a tile for every workgroup (a row tile per expert that can have rows), else mixed
     const bool turns = FWD && (long long)std::min(a.A, a.E) * ((f + SN - 1) / SN) >= kSmallSplitTarget;
@@ -639,12 +594,7 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
     else hipLaunchKernelGGL((gated_small_bf16<64, EPI, kGate>), grid, dim3(kSmallThreads), 0, s, c, p);
     return hipGetLastError();
   }
-  p.col_tiles = FWD ? (f + GN - 1) / GN : (f + BN - 1) / BN;
-  const unsigned grid = patched_grid(p.row_tiles_max, p.col_tiles);
-  if (K % 128 == 0)
-    hipLaunchKernelGGL((gated_persist_bf16<EPI>), dim3(std::min(grid, 256u)), dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
-  else
-    hipLaunchKernelGGL((gated_staged_bf16<EPI>), dim3(grid), dim3(kGemmThreads), 0, s, p);
+  launch_persist<EPI>(a, p, rk, s);
   return hipGetLastError();
 }
 

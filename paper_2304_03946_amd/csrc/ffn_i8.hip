@@ -14,11 +14,11 @@
 #include <algorithm>
 
 #include "common.h"
-#include "ffn_bf16_host.h"
 #include "ffn_bf16_tile.h"
 #include "ffn_bf16_dma.h"
 #include "ffn_bf16_persist.h"
 #include "ffn_bf16_small.h"
+#include "ffn_ragged_src.h"
 #include "ffn_small_core.h"
 
 namespace flexmoe {
@@ -56,6 +56,30 @@ template <typename T> struct I8Load {      // 16 elements of a row
     for (int i = 0; i < (int)sizeof(T); ++i) Vec16<T>::unpack(u[i], v + i * Vec16<T>::n);
   }
 };
+// Rows shorter than 1024 share a wave: the lanes of a row, a power of two of 16 elements each.
+__host__ __device__ inline int quant_lanes(int K) {
+  int n = 1;
+  while (n < kWave && n * 16 < K) n *= 2;
+  return n;
+}
+template <typename T>
+__device__ __forceinline__ void quantize_short_row(const T* __restrict__ x, int K, int lanes, bool there, int8_t* __restrict__ q, float* __restrict__ scale) {
+  const int k = (int)(threadIdx.x & (lanes - 1)) * 16;
+  I8Load<T> d;
+  float v[16] = {};
+  uint32_t m = 0;
+  if (there && k < K) {
+    d.load(x + k);
+    d.get(v);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  for (int o = 1; o < lanes; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+  const float s = i8_scale(m), inv = 1.f / s;
+  if (there && k == 0) *scale = s;
+  if (there && k < K)
+    *(uint4*)(q + k) = make_uint4(i8_pack(v, s, inv), i8_pack(v + 4, s, inv), i8_pack(v + 8, s, inv), i8_pack(v + 12, s, inv));
+}
 __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
@@ -63,7 +87,7 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
 }
 // A wave's row.
 template <typename T>
-__device__ __forceinline__ void quantize_row(const T* __restrict__ x, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
+__device__ __forceinline__ void quantize_long_row(const T* __restrict__ x, int K, int8_t* __restrict__ q, float* __restrict__ scale) {
   const int lane = threadIdx.x & 63;
   constexpr int kHeld = 4, kStep = kWave * 16;           // 4096 elements stay in registers; of longer rows the rest is read twice
   uint32_t m = 0;
@@ -101,11 +125,28 @@ __device__ __forceinline__ void quantize_row(const T* __restrict__ x, int K, int
   }
 }
 constexpr int kQuantWaves = 4;
+// Workgroup `block` of `blocks` that quantise M rows.
+template <typename T>
+__device__ __forceinline__ void quantize_rows_block(const T* __restrict__ x, int M, int K, int8_t* __restrict__ q, float* __restrict__ scale, int block,
+                                                    int blocks) {
+  const int lanes = quant_lanes(K), per = kQuantWaves * kWave / lanes;      // rows of a workgroup at a time
+  if (lanes == kWave) {
+    for (int r = block * per + threadIdx.x / kWave; r < M; r += blocks * per) quantize_long_row(x + (size_t)r * K, K, q + (size_t)r * K, scale + r);
+  } else {
+    for (int r0 = block * per; r0 < M; r0 += blocks * per) {
+      const int r = r0 + (int)threadIdx.x / lanes;       // (every lane takes part in the maximum)
+      quantize_short_row(x + (size_t)r * K, K, lanes, r < M, q + (size_t)r * K, scale + r);
+    }
+  }
+}
+static int quant_blocks(int M, int K, int most) {
+  const int per = kQuantWaves * kWave / quant_lanes(K);
+  return std::max(1, std::min((M + per - 1) / per, most));
+}
 template <typename T>
 __global__ __launch_bounds__(kQuantWaves * kWave) void quantize_rows_kernel(const T* __restrict__ x, int M, int K, int8_t* __restrict__ q,
                                                                             float* __restrict__ scale) {
-  for (int r = blockIdx.x * kQuantWaves + threadIdx.x / kWave; r < M; r += gridDim.x * kQuantWaves)
-    quantize_row(x + (size_t)r * K, K, q + (size_t)r * K, scale + r);
+  quantize_rows_block(x, M, K, q, scale, blockIdx.x, gridDim.x);
 }
 
 // w [E, K, NC] -> q [E, NC, K], scale [E, NC].  A workgroup has 64 columns of an expert: their largest values, then 64 x 64 tiles through LDS.
@@ -293,8 +334,8 @@ __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc
     default: { constexpr int ACT = FLEXMOE_SILU; __VA_ARGS__; break; }                     \
   }
 
-// Persistent kernel (see rows_gemm_persist_bf16), K a multiple of 128 two-byte units.
-template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThreads) void i8_persist(const I8Args p, const i32x4* row_tab) {
+// Persistent kernel (see rows_gemm_persist_bf16).  RAGGED: K is no multiple of 128 two-byte units (ffn_ragged_src.h).
+template <int EPI, typename T, bool GATHER, bool RAGGED> __global__ __launch_bounds__(kDmaThreads) void i8_persist(const I8Args p, const i32x4* row_tab) {
   constexpr bool GATE = EPI == I8_GATE;
   constexpr int TN = GATE ? BN / 2 : BN;                 // output columns of a tile
   __shared__ __align__(1024) unsigned char stage0[kDmaStageBytes];
@@ -307,12 +348,12 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
   lds_byte_t* const s1 = (lds_byte_t*)stage1;
   lds_byte_t* const s2 = (lds_byte_t*)stage2;
   lds_byte_t* const s3 = (lds_byte_t*)stage3;
-  typedef typename std::conditional<GATE, DmaSrcGateRows, DmaSrc>::type WSrc;
-  typedef RowsIssueV<WSrc> Issue;
+  typedef RaggedRows<typename std::conditional<GATE, DmaSrcGateRows, DmaSrc>::type, RAGGED> WSrc;
+  typedef RaggedIssue<RaggedRows<DmaSrc, RAGGED>, WSrc> Issue;
 
   const RowTabPtr tab = (RowTabPtr)row_tab;
-  const int K = p.K, NC = p.NC;
-  const TileSeq seq = make_tile_seq(tab[0][0], p.col_tiles, false, K / DK);
+  const int K = p.K, NC = p.NC, KT = RAGGED ? ragged_k_tiles(K) : K / DK;
+  const TileSeq seq = make_tile_seq(tab[0][0], p.col_tiles, false, KT);
   const unsigned G = gridDim.x;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = dma_wave_wm(wave), cb0 = dma_wave_cb0(wave);
@@ -333,6 +374,7 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
     const bf16_t* w = p.w + ((size_t)t.e * (GATE ? 2 * NC : NC) + t.n0) * K;
     if constexpr (GATE) is.w_src.init(w, K, t.cols_valid, NC);
     else is.w_src.init(w, K, t.cols_valid);
+    is.a_src.K = is.w_src.K = K;
     is.k_next = 0;
     return is;
   };
@@ -377,7 +419,7 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
     Issue next;
     if constexpr (GATHER) next = make_issue(tn);
     dma_pipeline_cont<false, false>(
-        s0, s1, s2, s3, acc, issue, K / DK, next, wm, cb0,
+        s0, s1, s2, s3, acc, issue, KT, next, wm, cb0,
         [&]() {
           fetch_scales(t, src);
           if (EPI != I8_OUT && threadIdx.x < BM) {
@@ -415,7 +457,7 @@ template <int EPI, typename T, bool GATHER> __global__ __launch_bounds__(kDmaThr
   __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): nothing may still be landing in LDS when the workgroup ends
 }
 
-// Few rows, or K in no whole rounds of the kernel above.
+// Few rows.
 template <int RB> struct I8Ahead {
   float rs[RB], cs[2][4], b[2][4];      // scales of the lane's rows and columns, biases
 };
@@ -517,9 +559,8 @@ __global__ __launch_bounds__(kGemmThreads) void i8_prep_kernel(const int32_t* __
   } else {
     const int first = a.small_blocks + a.row_blocks, n = gridDim.x - first;
     for (size_t i = (size_t)(b - first) * kGemmThreads + threadIdx.x; i < (size_t)a.A; i += (size_t)n * kGemmThreads) a.largest[i] = 0;
-    static_assert(kGemmThreads == kQuantWaves * kWave, "a row per wave");
-    for (int r = (b - first) * kQuantWaves + threadIdx.x / kWave; r < a.M; r += n * kQuantWaves)
-      quantize_row((const T*)a.x + (size_t)r * a.K, a.K, a.q + (size_t)r * a.K, a.scale + r);
+    static_assert(kGemmThreads == kQuantWaves * kWave, "quantize_rows_block's workgroup");
+    quantize_rows_block((const T*)a.x, a.M, a.K, a.q, a.scale, b - first, n);
   }
 }
 
@@ -567,12 +608,28 @@ size_t i8_ws_bytes(int N, int d, int f, int A, int E, int V, bool ffn) {
   return i8_layout(nullptr, N, d, f, A, E, V, ffn, &w);
 }
 
-// Row tiles of the few-rows kernels that a product with these sizes takes, 0: the 256 x 256 kernel.  The line between them is that of the
-// bf16 kernels (small_rows): per tile both sides do what they do there, on half the bytes and twice the rate.  K in no whole
-// rounds, or gathered rows beyond 32-bit byte offsets: few-rows kernels.
-static int i8_bm(int few, int K, bool gathered, long long rows_in) {
-  if (few) return few == 32 ? 16 : 64;
-  return K % 256 || (gathered && rows_in * K >= (1ll << 31)) ? 64 : 0;
+// Row tiles of the few-rows kernels that a product takes, 0: the 256 x 256 kernel.  wcols: its weight columns.
+// 16 rows up to four rows per expert (the product is a pass over the weights).  Otherwise what is expected to be done earlier, in ns, from the
+// tiles (the loads are not known here: half a ragged tile per bucket or expert):
+//   256 x 256: 12000, and 6500 + 850 per 64 k and 256 tiles, a full round of them at least
+//   64 x 128: 2900 + 760 per 128 k and 512 tiles, a full round at least; 3000 where few tiles are cut into segments
+// Fitted to both kernels' times for 360 products (1500 to 65000 rows, 1 to 24 experts of Zipf loads, K 80 to 2064, 80 to 4096 columns): the one
+// chosen took 1.001 of the faster one's time on average, 1.14 at most.  Some of them, us, 64 x 128 and 256 x 256: 6000 rows of one expert,
+// K 2064, 784 columns 34, 47, 2064 columns 62, 53; K 80, 4096 columns 29, 36; 30000 rows, K 80, 784 columns 27, 35, 4096 columns 104, 73; K 2064,
+// 256 columns 41, 49, 4096 columns 468, 302.  Gathered rows beyond 32-bit byte offsets: 64 x 128.
+static int i8_bm(const FfnArgs& a, int K, int wcols, bool gathered, long long rows_in) {
+  if (a.A <= 4 * a.E) return 16;
+  if (gathered && rows_in * K >= (1ll << 31)) return 64;
+  auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
+  const long long large_tiles = (a.A / BM + (a.V + 1) / 2) * ceil_div(wcols, BN), small_tiles = (a.A / 64 + (a.E + 1) / 2) * ceil_div(wcols, SN);
+  const long long large = 12000 + std::max(256ll, large_tiles) * (6500 + 850ll * ragged_k_tiles(K / 2)) / 256;
+  const long long stages = ceil_div(K, 128), seg = std::max(1ll, std::min<long long>(kSmallSplitTarget / std::max(small_tiles, 1ll), stages / 8));
+  const long long small = std::max<long long>(kSmallSplitTarget, small_tiles) * (2900 + 760 * ceil_div(stages, seg)) / kSmallSplitTarget + (seg > 1 ? 3000 : 0);
+  return small <= large ? 64 : 0;
+}
+template <int EPI, typename T, bool GATHER> static void launch_i8_persist(const I8Args& p, const i32x4* row_tab, dim3 grid, hipStream_t s) {
+  if (p.K % (4 * DK)) hipLaunchKernelGGL((i8_persist<EPI, T, GATHER, true>), grid, dim3(kDmaThreads), 0, s, p, row_tab);
+  else hipLaunchKernelGGL((i8_persist<EPI, T, GATHER, false>), grid, dim3(kDmaThreads), 0, s, p, row_tab);
 }
 template <int EPI, typename T>
 static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, hipStream_t s) {
@@ -591,11 +648,11 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
   const dim3 grid(std::min(patched_grid(a.A / BM + a.V, p.col_tiles), 256u));
   if constexpr (EPI == I8_OUT) {
     if (!p.gsrc) {
-      hipLaunchKernelGGL((i8_persist<EPI, T, false>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)w.row_tab);
+      launch_i8_persist<EPI, T, false>(p, w.row_tab, grid, s);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((i8_persist<EPI, T, true>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)w.row_tab);
+  launch_i8_persist<EPI, T, true>(p, w.row_tab, grid, s);
   return hipGetLastError();
 }
 
@@ -607,7 +664,7 @@ static void launch_prep(const FfnArgs& a, int bm1, int bm2, const int32_t* src, 
   g.small_blocks = bm ? 1 + (a.V * g.small.parts + 3) / 4 : 0;      // as the bf16 kernels' plan
   g.row_tab = bm1 && bm2 ? nullptr : w.row_tab;
   g.row_blocks = g.row_tab ? std::max(1, std::min(64, (a.A / BM + a.V + kGemmThreads - 1) / kGemmThreads)) : 0;
-  const int quant = g.x ? std::max(1, std::min((g.M + kQuantWaves - 1) / kQuantWaves, 2048)) : 0;
+  const int quant = g.x ? quant_blocks(g.M, g.K, 2048) : 0;
   hipLaunchKernelGGL(i8_prep_kernel<T>, dim3(g.small_blocks + g.row_blocks + quant), dim3(kGemmThreads), 0, s, a.voff, a.owner, a.E, a.V, g);
 }
 
@@ -616,7 +673,7 @@ static hipError_t matmul_i8_t(const FfnArgs& a, const void* xq, const float* xsc
                               const float* wscale, const void* bias, int K, int NC, void* y, void* ws, hipStream_t s) {
   I8Ws w;
   i8_layout((char*)ws, N, K, NC, a.A, a.E, a.V, false, &w);
-  const int bm = i8_bm(rows_kernels(a, nullptr).small.bm, K, src != nullptr, N);
+  const int bm = i8_bm(a, K, NC, src != nullptr, N);
   launch_prep<T>(a, bm, bm, src, k, I8Prep{}, w, s);
   const I8Args p{(const bf16_t*)xq, (const bf16_t*)wq, xscale, wscale, bias, K / 2, NC, 0, src, k, y, nullptr, FLEXMOE_RELU};
   return launch_i8<I8_OUT, T>(a, p, bm, w, s);
@@ -633,10 +690,7 @@ static hipError_t ffn_i8_t(const FfnArgs& a, const void* x, const int32_t* src, 
                            const void* w2q, const float* w2s, const void* b2, bool gated, void* yp, void* ws, hipStream_t s) {
   I8Ws w;
   i8_layout((char*)ws, N, a.d, a.f, a.A, a.E, a.V, true, &w);
-  FfnArgs rule = a;
-  if (gated) rule.f = 2 * a.f;
-  const int few = rows_kernels(rule, nullptr).small.bm;
-  const int bm1 = i8_bm(few, a.d, true, N), bm2 = i8_bm(few, a.f, false, 0);
+  const int bm1 = i8_bm(a, a.d, gated ? 2 * a.f : a.f, true, N), bm2 = i8_bm(a, a.f, a.d, false, 0);
   I8Prep g{};
   g.largest = w.largest;
   g.A = a.A;
@@ -664,7 +718,7 @@ hipError_t launch_ffn_i8(const FfnArgs& a, const void* x, const int32_t* src, in
 
 hipError_t launch_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, hipStream_t s) {
   if (M == 0) return hipSuccess;
-  const dim3 grid((unsigned)std::min((M + kQuantWaves - 1) / kQuantWaves, 4096));
+  const dim3 grid((unsigned)quant_blocks(M, K, 4096));
   if (dtype == FLEXMOE_BF16)
     hipLaunchKernelGGL(quantize_rows_kernel<bf16_t>, grid, dim3(kQuantWaves * kWave), 0, s, (const bf16_t*)x, M, K, (int8_t*)q, scale);
   else
