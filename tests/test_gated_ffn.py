@@ -17,6 +17,15 @@ import torch
 ACTS = ("relu", "gelu_erf", "gelu_tanh", "silu")
 
 
+@pytest.fixture(autouse=True)
+def float32_by_default():
+    """Another module may have left float64 as the default type."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def _b():
     from paper_2304_03946_amd import binding as B
     B.load_library()

@@ -11,7 +11,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gated_ffn import act64, buckets, split
+from test_gated_ffn import act64, buckets, float32_by_default, split  # noqa: F401
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 TINY = 2.0 ** -126
