@@ -465,15 +465,13 @@ __global__ __launch_bounds__(kF32Threads, 2) void rows_gated_f32(const float* __
 // dW_e[m, n] = sum over the vExperts v of e (ascending v), rows p of v: L[p, m] * R[p, n].  The rows of all of the
 // expert's buckets are one contraction: K tile kt holds rows 32 kt .. of the buckets laid behind each other.  Output rows from m_first on.
 template <int MT>
-__global__ __launch_bounds__(kF32Threads, 2) void wgrad_f32(const float* __restrict__ L, const float* __restrict__ R,
-                                                            const int32_t* __restrict__ voff,
-                                                            const int32_t* __restrict__ owner, int V, int M, int NC,
-                                                            int m_first, float* __restrict__ dw) {
+__device__ __forceinline__ void wgrad_f32_block(const float* __restrict__ L, const float* __restrict__ R, const int32_t* __restrict__ voff,
+                                                const int32_t* __restrict__ owner, int V, int M, int NC, int e, int m0, int n0,
+                                                float* __restrict__ dw) {
   typedef F32Loop<MT, false, false> Loop;
   __shared__ __align__(1024) unsigned char smem[Loop::kLds];
   __shared__ int s_first[FLEXMOE_MAX_VEXPERTS], s_end[FLEXMOE_MAX_VEXPERTS];      // first row - rows before it, rows up to its end
   __shared__ int s_n;
-  const int e = blockIdx.z, m0 = m_first + (int)blockIdx.y * (MT * 32), n0 = blockIdx.x * FN;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (wave == 0) {                  // the expert's non-empty buckets, ascending
     int n = 0, total = 0;
@@ -588,6 +586,31 @@ __global__ __launch_bounds__(kF32Threads, 2) void wgrad_f32(const float* __restr
     if (m < M && col < NC && (MT == 2 || j == (wave >> 1)))
       *(float4*)(dw + (size_t)e * M * NC + (size_t)m * NC + col) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
   }
+}
+
+template <int MT>
+__global__ __launch_bounds__(kF32Threads, 2) void wgrad_f32(const float* __restrict__ L, const float* __restrict__ R,
+                                                            const int32_t* __restrict__ voff,
+                                                            const int32_t* __restrict__ owner, int V, int M, int NC,
+                                                            int m_first, float* __restrict__ dw) {
+  wgrad_f32_block<MT>(L, R, voff, owner, V, M, NC, blockIdx.z, m_first + (int)blockIdx.y * (MT * 32), blockIdx.x * FN, dw);
+}
+// Both gradients of gated experts in one launch, a workgroup per tile of either: where one product's tiles leave compute units without work the
+// other's run there (11318 rows of 2 experts, d 120, f 224: 24 and 40 tiles).
+struct GradF32 {
+  const float* L;
+  const float* R;
+  float* dw;
+  int M, NC, m_tiles, n_tiles;
+};
+template <int MT>
+__global__ __launch_bounds__(kF32Threads, 2) void wgrad_pair_f32(GradF32 g0, GradF32 g1, const int32_t* __restrict__ voff,
+                                                                 const int32_t* __restrict__ owner, int V, unsigned first1) {
+  const bool second = blockIdx.x >= first1;
+  const GradF32 g = second ? g1 : g0;
+  const unsigned b = blockIdx.x - (second ? first1 : 0u), per = (unsigned)g.m_tiles * (unsigned)g.n_tiles, t = b % per;
+  wgrad_f32_block<MT>(g.L, g.R, voff, owner, V, g.M, g.NC, (int)(b / per), (int)(t / (unsigned)g.n_tiles) * (MT * 32), (int)(t % (unsigned)g.n_tiles) * FN,
+                      g.dw);
 }
 
 static unsigned tiles_of(int n, int t) { return (unsigned)((n + t - 1) / t); }
@@ -708,8 +731,20 @@ hipError_t launch_ffn_gated_bwd_f32(const FfnArgs& a, const void* dyp, const voi
     launch_gated_f32<EPI_DH>(a, dyp, w2, nullptr, hpre, dhpre, h_kept ? nullptr : h_ws, s);
     launch_rows_f32<true, EPI_PLAIN>(a, dhpre, w1, nullptr, 2 * a.f, a.d, nullptr, dxp, nullptr, s);
   }
-  launch_wgrad_f32(a, h_kept ? (const float*)h_kept : h_ws, dyp, a.f, a.d, dw2, s);
-  launch_wgrad_f32(a, xp, dhpre, a.d, 2 * a.f, dw1, s);
+  const float* h = h_kept ? (const float*)h_kept : h_ws;
+  // (sums do not depend on the tiles' height)
+  const int mt = f32_wgrad_blocks(a, a.d, 3 * a.f);
+  const GradF32 g0{h, (const float*)dyp, (float*)dw2, a.f, a.d, (int)tiles_of(a.f, mt * 32), (int)tiles_of(a.d, FN)};
+  const GradF32 g1{(const float*)xp, dhpre, (float*)dw1, a.d, 2 * a.f, (int)tiles_of(a.d, mt * 32), (int)tiles_of(2 * a.f, FN)};
+  const long long b0 = (long long)a.E * g0.m_tiles * g0.n_tiles, b1 = (long long)a.E * g1.m_tiles * g1.n_tiles;
+  if ((b0 + b1) * kF32Threads < (1ll << 32)) {
+    const dim3 grid((unsigned)(b0 + b1));
+    if (mt == 2) hipLaunchKernelGGL(wgrad_pair_f32<2>, grid, dim3(kF32Threads), 0, s, g0, g1, a.voff, a.owner, a.V, (unsigned)b0);
+    else hipLaunchKernelGGL(wgrad_pair_f32<1>, grid, dim3(kF32Threads), 0, s, g0, g1, a.voff, a.owner, a.V, (unsigned)b0);
+  } else {                                           // more than a launch takes
+    launch_wgrad_f32(a, h, dyp, a.f, a.d, dw2, s);
+    launch_wgrad_f32(a, xp, dhpre, a.d, 2 * a.f, dw1, s);
+  }
   return hipGetLastError();
 }
 
