@@ -168,7 +168,7 @@ int flexmoe_expert_ffn_bwd_top1(const void* dyp, const void* xp, const void* hpr
  * the fp32 number), each rounded to the nearest.
  * ws: at least flexmoe_workspace_bytes(N, d, 2 * f, E, k, V, dtype) bytes, as for flexmoe_expert_ffn_gated_bwd.
  * d and f are multiples of 8 below 2^20.  Equal calls give equal bits; as in flexmoe_expert_ffn_fwd, a row's last bits may depend on the
- * bucket sizes.
+ * bucket sizes.  No output of this call, of its backward pass or of the 8-bit calls below may overlap an input, another output or ws.
  */
 int flexmoe_expert_ffn_gated_fwd(const void* xp, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1,
                                  const void* b1, const void* w2, const void* b2, int A, int d, int f, int E, int V, int act,

@@ -252,6 +252,24 @@ def test_many_rows_fp32(A, d, f, E, V):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_past_32_bits(dtype):
+    """Hpre of more than 2^31 elements: the rows of the last expert, behind that point, against the formulas."""
+    A, d, f, last = 270_000, 64, 4096, 400
+    c = Case(A, d, f, 2, 2, dtype, "silu", True, seed=9, counts=[A - last, last])
+    c.owner.copy_(torch.arange(2))
+    assert c.hpre.numel() > 2 ** 31 and (A - last) * 2 * f > 2 ** 31
+    c.fwd()
+    c.bwd()
+    names = ("x", "dy", "hpre", "h", "y", "dxp")
+    c.__dict__.update({n: getattr(c, n)[-last:] for n in names})
+    c.__dict__.update({n: getattr(c, n)[1:] for n in ("w1", "w2", "b1", "b2", "dw1", "dw2")})
+    c.rows = torch.zeros(last, dtype=torch.long, device="cuda")
+    c.check_fwd()
+    c.check_bwd(True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("A,d,f", [(90, 64, 72), (7300, 2048, 1024)])
 def test_bias_gradients(A, d, f, dtype):
     """flexmoe_expert_bias_grads with 2 f in the place of f reads dHpre where the backward call left it."""

@@ -130,7 +130,7 @@ def check_product(y, q, s, wq, ws, bias, rows, expert, dtype):
 
 
 # tokens, K, NC, experts, per token, vExperts: one row; few rows with and without segments; K in no whole stages; 256 x 256 tiles, K in whole
-# rounds of 256 and not (few-rows kernels then); one expert
+# rounds of 256 and not; one expert
 PRODUCTS = [(1, 16, 8, 1, 1, 1), (3, 64, 72, 4, 2, 5), (16, 2048, 512, 8, 2, 12), (130, 336, 912, 12, 3, 15), (900, 272, 256, 4, 1, 9),
             (2500, 2048, 2056, 4, 3, 6), (7300, 2048, 1000, 3, 1, 3), (7300, 2064, 1024, 3, 1, 3), (7300, 2048, 2048, 1, 1, 1)]
 
@@ -254,19 +254,59 @@ def test_ffn(N, d, f, E, k, V, gated, act, bias, dtype):
 
 
 @pytest.mark.gpu
-def test_a_row_depends_on_nothing_else():
+@pytest.mark.parametrize("act,gated", [("silu", True), ("gelu_erf", True), ("gelu_tanh", False), ("relu", False)])
+def test_a_row_depends_on_nothing_else(act, gated):
     """The same bits for a token alone, in a few-rows batch and in a large one."""
-    big = Ffn(4000, 2048, 1024, 4, 2, 6, True, "silu", "bf16", True, seed=4)
+    big = Ffn(4000, 2048, 1024, 4, 2, 6, gated, act, "bf16", True, seed=4)
     y = big.run().clone()
+    shared = ("w1", "s1", "b1", "w2", "s2", "b2")
     at = torch.nonzero(big.t.token == 17).flatten()
     for p in at.tolist():
-        one = Ffn(1, 2048, 1024, 4, 1, 4, True, "silu", "bf16", True, seed=4)
+        one = Ffn(1, 2048, 1024, 4, 1, 4, gated, act, "bf16", True, seed=4)
         e = int(big.t.expert[p])
-        one.x, one.w1, one.s1, one.b1, one.w2, one.s2, one.b2 = big.x[17:18].clone(), big.w1, big.s1, big.b1, big.w2, big.s2, big.b2
+        one.x = big.x[17:18].clone()
+        one.__dict__.update({n: getattr(big, n) for n in shared})
         one.t.owner = torch.arange(4, dtype=torch.int32, device="cuda")
         one.t.voff = (torch.arange(5, device="cuda") > e).int()
         one.t.src = torch.zeros(1, dtype=torch.int32, device="cuda")
         assert torch.equal(one.run()[0], y[p])
+    some = Ffn(130, 2048, 1024, 4, 2, 6, gated, act, "bf16", True, seed=5)
+    some.x = big.x[:130].clone()
+    some.__dict__.update({n: getattr(big, n) for n in shared})
+    some.run()
+    where = {(t, e): p for p, (t, e) in enumerate(zip(big.t.token.tolist(), big.t.expert.tolist()))}
+    both = [(p, where[te]) for p, te in enumerate(zip(some.t.token.tolist(), some.t.expert.tolist())) if te in where]
+    assert len(both) > 40
+    here, there = torch.tensor(both, device="cuda").T
+    assert torch.equal(some.y[here], y[there])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("M,K,NC", [(540_000, 4096, 64), (540_000, 64, 4096)])
+def test_offsets_past_32_bits(M, K, NC, gather):
+    """Rows and outputs of more than 2^31 elements: the last rows as in a call of their own, bit for bit; their integers too."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(M)
+    B, last = _b(), 300
+    x = torch.randn(M, K, generator=gen, device="cuda", dtype=torch.bfloat16)
+    q, s = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    B.flexmoe_quantize_rows(x, q, s)
+    ql, sl = torch.empty(last, K, dtype=torch.int8, device="cuda"), torch.empty(last, device="cuda")
+    B.flexmoe_quantize_rows(x[-last:].contiguous(), ql, sl)
+    assert torch.equal(ql, q[-last:]) and torch.equal(sl, s[-last:])
+    del x
+    wq, ws = weights(2, NC, K, gen)
+    own = torch.arange(2, dtype=torch.int32, device="cuda")
+
+    def product(q, s, first):
+        n = len(q)
+        y = torch.empty(n, NC, dtype=torch.bfloat16, device="cuda")
+        work = torch.empty(B.flexmoe_i8_workspace_bytes(n, 16, 16, 2, 1, 2, 0), dtype=torch.uint8, device="cuda")
+        off = torch.tensor([0, first, n], dtype=torch.int32, device="cuda")
+        B.flexmoe_expert_matmul_i8(q, s, torch.arange(n, dtype=torch.int32, device="cuda") if gather else None, 1, off, own, wq, ws, None, y, work)
+        return y
+    assert torch.equal(product(q, s, M - last + 100)[-last:], product(ql, sl, 100))
 
 
 @pytest.mark.gpu
