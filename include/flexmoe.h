@@ -168,7 +168,7 @@ int flexmoe_expert_ffn_bwd_top1(const void* dyp, const void* xp, const void* hpr
  * the fp32 number), each rounded to the nearest.
  * ws: at least flexmoe_workspace_bytes(N, d, 2 * f, E, k, V, dtype) bytes, as for flexmoe_expert_ffn_gated_bwd.
  * d and f are multiples of 8 below 2^20.  Equal calls give equal bits; as in flexmoe_expert_ffn_fwd, a row's last bits may depend on the
- * bucket sizes.  No output of this call, of its backward pass or of the 8-bit calls below may overlap an input, another output or ws.
+ * bucket sizes.
  */
 int flexmoe_expert_ffn_gated_fwd(const void* xp, const int32_t* vexpert_off, const int32_t* vexpert_owner, const void* w1,
                                  const void* b1, const void* w2, const void* b2, int A, int d, int f, int E, int V, int act,
@@ -198,6 +198,7 @@ int flexmoe_expert_ffn_gated_bwd(const void* dyp, const void* xp, const void* hp
  * flexmoe_quantize_weights: the same for every output channel of w [E,K,NC] dtype (flexmoe_expert_ffn_fwd's layout)
  *   -> q [E,NC,K] int8 (the contraction contiguous), scale [E,NC].  Done once per set of weights.
  * K is a multiple of 16, NC of 8; K < 2^20 (rows), K < 2^17, NC < 2^20 and K * NC < 2^31 (weights, and every call below).
+ * No output of the 8-bit calls may overlap an input, another output or ws.
  */
 int flexmoe_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, void* stream);
 int flexmoe_quantize_weights(const void* w, int E, int K, int NC, int dtype, void* q, float* scale, void* stream);

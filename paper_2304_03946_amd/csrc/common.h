@@ -138,6 +138,9 @@ typedef PlacementArgT<FLEXMOE_MAX_EXPERTS, FLEXMOE_MAX_VEXPERTS> PlacementArg;
 typedef PlacementArgT<64, 128> PlacementArgSmall;
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool overlap(const void* p, const void* q, size_t bytes_p, size_t bytes_q) {
+  return (uintptr_t)p < (uintptr_t)q + bytes_q && (uintptr_t)q < (uintptr_t)p + bytes_p;
+}
 
 // ---- launchers (host side; each returns hipGetLastError() of its launches) ----
 size_t gate_ws_bytes(int d, int E, int dtype);

@@ -436,10 +436,6 @@ static void launch_wgrad_reduce(const FfnArgs& a, const WgradDmaArgs* g, int n, 
   hipLaunchKernelGGL(wgrad_reduce_kernel, dim3(blocks, a.E, n), dim3(kGemmThreads), 0, s, r);
 }
 
-static bool overlap(const void* p, const void* q, size_t bytes_p, size_t bytes_q) {
-  return (uintptr_t)p < (uintptr_t)q + bytes_q && (uintptr_t)q < (uintptr_t)p + bytes_p;
-}
-
 // dXp = dHpre . W1^T (W1_e is [d, f], contraction index f contiguous), dW2 = H^T . dYp, dW1 = Xp^T . dHpre: the weight gradients
 // each with its own partial tiles.  In this order, so that a caller who needs w1, h or dyp no longer may have a gradient written over
 // them: products that share a launch only do where the later one's output is nothing that the earlier one reads.

@@ -737,11 +737,14 @@ hipError_t launch_ffn_gated_bwd_f32(const FfnArgs& a, const void* dyp, const voi
   const GradF32 g0{h, (const float*)dyp, (float*)dw2, a.f, a.d, (int)tiles_of(a.f, mt * 32), (int)tiles_of(a.d, FN)};
   const GradF32 g1{(const float*)xp, dhpre, (float*)dw1, a.d, 2 * a.f, (int)tiles_of(a.d, mt * 32), (int)tiles_of(2 * a.f, FN)};
   const long long b0 = (long long)a.E * g0.m_tiles * g0.n_tiles, b1 = (long long)a.E * g1.m_tiles * g1.n_tiles;
-  if ((b0 + b1) * kF32Threads < (1ll << 32)) {
+  // (a caller who needs h or dyp no longer may have dW1 written over them: then it comes last)
+  const size_t w1_bytes = (size_t)a.E * a.d * 2 * a.f * sizeof(float), row_bytes = (size_t)a.A * sizeof(float);
+  const bool joint = !overlap(dw1, h, w1_bytes, row_bytes * a.f) && !overlap(dw1, dyp, w1_bytes, row_bytes * a.d);
+  if (joint && (b0 + b1) * kF32Threads < (1ll << 32)) {
     const dim3 grid((unsigned)(b0 + b1));
     if (mt == 2) hipLaunchKernelGGL(wgrad_pair_f32<2>, grid, dim3(kF32Threads), 0, s, g0, g1, a.voff, a.owner, a.V, (unsigned)b0);
     else hipLaunchKernelGGL(wgrad_pair_f32<1>, grid, dim3(kF32Threads), 0, s, g0, g1, a.voff, a.owner, a.V, (unsigned)b0);
-  } else {                                           // more than a launch takes
+  } else {
     launch_wgrad_f32(a, h, dyp, a.f, a.d, dw2, s);
     launch_wgrad_f32(a, xp, dhpre, a.d, 2 * a.f, dw1, s);
   }

@@ -252,6 +252,29 @@ def test_many_rows_fp32(A, d, f, E, V):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("A,d,f", [(90, 64, 72), (1600, 136, 264), (7300, 1024, 512)])
+def test_weight_gradients_over_what_is_read_no_longer(A, d, f, dtype):
+    """dXp, dW2, dW1 are computed in this order, behind dHpre: what they have read may be overwritten by what comes later."""
+    c = Case(A, d, f, 2, 3, dtype, "silu", False, seed=5)
+    c.fwd()
+    c.bwd()
+    outs = ("dxp", "dw1", "dw2")
+    want = {n: getattr(c, n).clone() for n in outs}
+    kept = {n: getattr(c, n).clone() for n in ("w1", "w2", "hpre", "h", "dy", *outs)}
+    for grad, over in (("dw1", "w1"), ("dw2", "w1"), ("dw1", "w2"), ("dw2", "w2"), ("dw1", "h"), ("dw1", "dy"), ("dw1", "hpre")):
+        c.__dict__.update({n: t.clone() for n, t in kept.items()})
+        g, t = getattr(c, grad), getattr(c, over)
+        room = torch.empty(max(g.numel(), t.numel()), dtype=c.dt, device="cuda")
+        room[:t.numel()] = t.flatten()
+        setattr(c, over, room[:t.numel()].view(t.shape))
+        setattr(c, grad, room[:g.numel()].view(g.shape))
+        c.bwd()
+        for n in outs:
+            assert torch.equal(getattr(c, n), want[n]), (grad, over, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_offsets_past_32_bits(dtype):
     """Hpre of more than 2^31 elements: the rows of the last expert, behind that point, against the formulas."""
     A, d, f, last = 270_000, 64, 4096, 400
