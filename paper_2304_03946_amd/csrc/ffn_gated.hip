@@ -18,7 +18,9 @@
 // bits more than bf16 has (keep4): as bf16 they put as much error into the gradients as the rounding of dHpre that cannot be
 // avoided (rel. error of dW1 and dX, 64-bit formula: 0.0030 with bf16 words, 0.0024 with these, 0.0017 is the rounding of the output alone).
 //
-// What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.
+// What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.  Measured:
+// 32768 tokens x 2, d 2048, f 5632, 32 experts: first product 2.86 ms (1.06 PFLOP/s), Y 1.25 (1.21), dH 1.75 (0.87), dX 2.68 (1.13), both weight
+// gradients 4.43 (1.02); a large library product runs at 1.42.  16 tokens x 2, d 1024, f 4096, 17 experts with rows: 427 MB of weights in 89 us.
 #include <algorithm>
 
 #include "common.h"

@@ -10,7 +10,11 @@
 // epilogue makes H = act(z) or act(g) * u in fp32, stores it in the layer's dtype and takes the largest |H| of every row (before that
 // rounding) with integer atomics on its bits -- a maximum does not depend on their order; a pass over H makes its integers, and the second
 // product reads them.  H has to be complete before its row's scale is known, so it goes through memory once as dtype and once as integers:
-// 5 bytes per element of the FFN's 2 K operations each (bf16).
+// 6 bytes per element (bf16): 0.21 of 2.53 ms at 32768 tokens x 2, d 2048, f 5632.
+//
+// What bounds them: the matrix cores at hundreds of rows per expert (there, gated, both products 2.0 Pop/s; a large library product reaches
+// 2.47), the weights' bytes at few (48 tokens x 2, d 2048, f 4096, 64 experts: 1.0 GB in 213 us), launches and first loads between (one token
+// x 2, d 1024, f 4096: 4.0, 11.9, 4.0 and 7.7 us).
 #include <algorithm>
 
 #include "common.h"
