@@ -151,6 +151,7 @@ __device__ __forceinline__ void gated_fwd_rounds(lds_byte_t* patch, const DmaAcc
 #pragma unroll
   for (int round = 0; round < 2 * MB; ++round) {
     const int i = round >> 1, sub = round & 1;
+    if (!FULL && (wm + 2 * i) * 32 + sub * 16 >= t.rows_valid) break;      // (a bucket's last tile: no rows from here on)
     typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
     float gu[2][2][4];                                   // [G, U][sj]
     uint32_t other = 0;
@@ -256,6 +257,7 @@ __device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaA
   write_round(0, 0);
 #pragma unroll
   for (int round = 0; round < kRounds; ++round) {
+    if (!FULL && (wm + round / 2 * 2) * 32 + round % 2 * 16 >= t.rows_valid) break;
     if (round + kAhead < kRounds) fetch_round(round + kAhead);
     asm volatile("" ::: "memory");
     float4 v[kIts];
@@ -307,6 +309,7 @@ __device__ __forceinline__ void gated_plain_rounds(lds_byte_t* patch, const DmaA
 #pragma unroll
   for (int round = 0; round < 2 * MB; ++round) {
     const int i = round >> 1, sub = round & 1;
+    if (!FULL && (wm + 2 * i) * 32 + sub * 16 >= t.rows_valid) break;
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj)
 #pragma unroll

@@ -281,6 +281,7 @@ __device__ __forceinline__ void i8_rounds(lds_byte_t* patch, const DmaAccI8& acc
   for (int round = 0; round < 2 * MB; ++round) {
     const int i = round >> 1, sub = round & 1;
     const int row0 = (wm + 2 * i) * 32 + sub * 16;       // of the tile
+    if (!FULL && row0 >= t.rows_valid) break;
     const float rs = row_scale[row0 + r];
     uint32_t most = 0;
 #pragma unroll
