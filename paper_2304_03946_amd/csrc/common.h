@@ -167,6 +167,7 @@ struct FfnArgs {
   int A, d, f, E, V, act;
   const int32_t* voff;
   const int32_t* owner;
+  char* few_ws = nullptr;        // bf16: room for the few-rows kernels' tables where they are taken past their own line (gated experts), or null
 };
 size_t ffn_ws_bytes(int A, int d, int f, int E, int V, int dtype);
 // h_keep / h_kept: act(Hpre) in a buffer of the caller's (written by the forward pass, read by the backward pass), or null

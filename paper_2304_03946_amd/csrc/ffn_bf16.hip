@@ -207,8 +207,9 @@ static int small_rows(int A, int d, int f, int E, int V) {
 // rows (480) 224, 221; d 1024, f 2048, E 8, 2048 rows 100, 96; the ratio over 120 layers inside the lines 0.75 - 0.98.
 // Past the lines: d 1024, f 2048, E 8, 5120 rows (704 tiles) 191, 193; d 512, f 1024, E 128 (8192
 // tiles of weight gradients), 4096 rows 219, 224; d 1024, f 4096, E 32 (16384), 1024 rows 284, 294; d 2048, f 8192, E 64, 2048 rows 1835, 1951.
+static int small_rows(const FfnArgs& a) { return a.few_ws ? 64 : small_rows(a.A, a.d, a.f, a.E, a.V); }
 static bool bwd_products_merged(const FfnArgs& a) {
-  if (!small_rows(a.A, a.d, a.f, a.E, a.V) || !wgrad_small(a.A, a.d, a.f, a.E)) return false;
+  if (!small_rows(a) || !wgrad_small(a.A, a.d, a.f, a.E)) return false;
   const long long d_tiles = (a.d + GT - 1) / GT, f_tiles = (a.f + GT - 1) / GT;
   return (a.A / 64 + a.E) * d_tiles <= kSmallSplitTarget && 2 * a.E * d_tiles * f_tiles <= 6144;
 }
@@ -256,9 +257,9 @@ static i32x4* rows_tab_ws(const FfnArgs& a, void* ws) { return (i32x4*)((char*)r
 static int small_plan_parts(const FfnArgs& a) { return std::max(1, std::min(a.A / (a.V * 512), 2048 / a.V)); }      // waves per bucket, up to 512 workgroups
 static SmallPlan small_plan_ws(const FfnArgs& a, void* ws, float** partial = nullptr) {
   SmallPlan pl;
-  pl.bm = small_rows(a.A, a.d, a.f, a.E, a.V);
+  pl.bm = small_rows(a);
   pl.parts = small_plan_parts(a);
-  char* at = (char*)rows_ws(a, ws);
+  char* at = a.few_ws ? a.few_ws : (char*)rows_ws(a, ws);
   pl.tab = (i32x4*)at;
   at += small_tab_bytes(a.A, a.E);
   pl.rowmap = (int32_t*)at;
@@ -269,7 +270,7 @@ static SmallPlan small_plan_ws(const FfnArgs& a, void* ws, float** partial = nul
   return pl;
 }
 static int plan_blocks(const FfnArgs& a) {
-  if (small_rows(a.A, a.d, a.f, a.E, a.V)) return 1 + (a.V * small_plan_parts(a) + 3) / 4;      // the first: row tiles; the others: the row list
+  if (small_rows(a)) return 1 + (a.V * small_plan_parts(a) + 3) / 4;      // the first: row tiles; the others: the row list
   return std::max(1, std::min(64, (max_row_tiles(a.A, a.V) + kGemmThreads - 1) / kGemmThreads));
 }
 // What the rows kernels of one forward call look up: the row-tile table of the persistent kernels, or the small kernels'
@@ -280,10 +281,15 @@ void launch_rows_plan(const FfnArgs& a, void* ws, hipStream_t s) {
   else hipLaunchKernelGGL(rows_plan_kernel, dim3(plan_blocks(a)), dim3(kGemmThreads), 0, s, a.voff, a.owner, a.V, rows_tab_ws(a, ws));
 }
 
+static long long small_slots(const FfnArgs& a, int bm) { return std::max(small_slots(a.A, a.E, bm, a.d, a.f), small_slots(a.A, a.E, bm, a.f, a.d)); }
+size_t few_tables_bytes(const FfnArgs& a) {
+  return small_tab_bytes(a.A, a.E) + align_up((size_t)a.A * sizeof(int32_t), 256) + align_up(kSmallSlots * sizeof(int), 256) +
+         (size_t)small_slots(a, 64) * 64 * SN * sizeof(float);
+}
 RowsKernels rows_kernels(const FfnArgs& a, void* ws) {
   RowsKernels r;
   r.small = small_plan_ws(a, ws, &r.small_partial);
-  r.small_slots = r.small.bm ? (int)std::max(small_slots(a.A, a.E, r.small.bm, a.d, a.f), small_slots(a.A, a.E, r.small.bm, a.f, a.d)) : 0;
+  r.small_slots = r.small.bm ? (int)small_slots(a, r.small.bm) : 0;
   r.row_tab = rows_tab_ws(a, ws);
   return r;
 }
@@ -376,7 +382,7 @@ static hipError_t launch_rows(const FfnArgs& a, const void* in, const void* w, c
                               const void* hpre_in, void* out0, void* out1, void* ws, hipStream_t s,
                               const int32_t* gsrc = nullptr, int gk = 1, void* split_ws = nullptr,
                               const int32_t* scatter_rows = nullptr) {
-  if (small_rows(a.A, a.d, a.f, a.E, a.V)) return launch_small<WT, EPI>(a, in, w, bias, K, NC, hpre_in, out0, out1, ws, s, gsrc, gk, scatter_rows);
+  if (small_rows(a)) return launch_small<WT, EPI>(a, in, w, bias, K, NC, hpre_in, out0, out1, ws, s, gsrc, gk, scatter_rows);
   const i32x4* tab = rows_tab_ws(a, ws);
   if (EPI == EPI_PLAIN)
     return launch_rows_t<WT, EPI, FLEXMOE_RELU>(a, in, w, bias, K, NC, hpre_in, out0, out1, s, gsrc, gk, split_ws,
@@ -440,6 +446,7 @@ static void launch_wgrad_reduce(const FfnArgs& a, const WgradDmaArgs* g, int n, 
 // each with its own partial tiles.  In this order, so that a caller who needs w1, h or dyp no longer may have a gradient written over
 // them: products that share a launch only do where the later one's output is nothing that the earlier one reads.
 // fh: columns of H and rows of dW2 -- a.f, or half of it where dHpre holds two gradients for each of H's columns (gated experts).
+// dxp null: there already.
 hipError_t launch_bwd_products(const FfnArgs& a, int fh, const void* h, const void* dyp, void* dw2, const void* xp, const void* dhpre,
                                void* dw1, const void* w1, void* dxp, const int32_t* scatter_src, void* ws, hipStream_t s) {
   void* tail2 = (char*)ws + 2 * align_up((size_t)a.A * a.f * sizeof(bf16_t), 256);
@@ -451,7 +458,7 @@ hipError_t launch_bwd_products(const FfnArgs& a, int fh, const void* h, const vo
   const size_t row_bytes = (size_t)a.A * sizeof(bf16_t);
   const bool joint = wgrad_joint(grid[0], grid[1]) && !overlap(dw1, h, w_bytes, row_bytes * fh) && !overlap(dw1, dyp, w_bytes, row_bytes * a.d);
   const WgradSmallArgs both{{g[0], g[1]}, grid[0]};
-  if (a.A > 0 && joint && bwd_products_merged(a) && !overlap(dw1, w1, w_bytes, w_bytes) && !overlap(dw2, w1, w2_bytes, w_bytes)) {
+  if (a.A > 0 && dxp && joint && bwd_products_merged(a) && !overlap(dw1, w1, w_bytes, w_bytes) && !overlap(dw2, w1, w2_bytes, w_bytes)) {
     int bm;
     unsigned rows_grid;
     const SmallArgs p = small_args<EPI_PLAIN>(a, dhpre, w1, nullptr, a.f, a.d, nullptr, dxp, nullptr, ws, nullptr, 1, scatter_src, &bm, &rows_grid);
@@ -462,7 +469,7 @@ hipError_t launch_bwd_products(const FfnArgs& a, int fh, const void* h, const vo
     launch_wgrad_reduce(a, g, 2, s);
     return hipGetLastError();
   }
-  if (a.A > 0) {
+  if (a.A > 0 && dxp) {
     const hipError_t err = launch_rows<true, EPI_PLAIN>(a, dhpre, w1, nullptr, a.f, a.d, nullptr, dxp, nullptr, ws, s, nullptr, 1,
                                                         rows_split_ws(a, ws), scatter_src);
     if (err != hipSuccess) return err;

@@ -11,8 +11,8 @@
 //  * a tile of the first product holds a column of G and the same column of U in the same lane: its weight columns are taken from the two
 //    halves of W1 in turn, 32 and 32.  Only the addresses of the weights' loads know about it.
 //  * G, U and H leave through a wave-private LDS patch as bf16 (half of what fp32 patches move): 16 bytes per lane, 64 per row.
-//  * two sets of kernels, chosen as for an ungated layer with 2 f columns: 256 x 256 tiles with direct-to-LDS loads for any K (a contraction
-//    that is no multiple of 128 ends in zeros, ffn_ragged_src.h; Y's product is here as well for such f), and 32- or 64-row tiles for few
+//  * two sets of kernels (chosen in `doubled`): 256 x 256 tiles with direct-to-LDS loads for any K (a contraction
+//    that is no multiple of 128 ends in zeros, ffn_ragged_src.h; Y's and dX's products are here as well for such f), and 32- or 64-row tiles for few
 //    rows (small_core).
 // Rounding: H is made of the fp32 sums and rounded once.  What is kept of G and U for the backward pass are 16-bit words with two mantissa
 // bits more than bf16 has (keep4): as bf16 they put as much error into the gradients as the rounding of dHpre that cannot be
@@ -82,6 +82,7 @@ __device__ __forceinline__ void kept4(uint2 w, float* v) {
   v[3] = kept_low(w.y >> 16);
 }
 
+constexpr int EPI_PLAIN_T = 4;
 struct GatedArgs {
   const bf16_t* in;              // fwd: Xp, dH: dYp
   const bf16_t* w;               // fwd: W1 [E, d, 2 f], dH: W2 [E, f, d]
@@ -364,7 +365,8 @@ __device__ __forceinline__ void gated_epilogue(unsigned char* stage, const DmaAc
   }
 
 // The persistent kernel of these products (see rows_gemm_persist_bf16): 256 workgroups walk the tiles, the next tile's first loads go out
-// while the current K loop drains.  EPI_FWD1: a tile is 256 rows x 128 columns of H; EPI_DH, EPI_DHQ: 256 of dH; EPI_PLAIN: 256 of Y.
+// while the current K loop drains.  EPI_FWD1: a tile is 256 rows x 128 columns of H; EPI_DH, EPI_DHQ: 256 of dH; EPI_PLAIN: 256 of Y,
+// EPI_PLAIN_T: of dX (W1 [d, 2 f], the contraction contiguous).
 template <int EPI, bool RAGGED> __global__ __launch_bounds__(kDmaThreads) void gated_persist_bf16(const GatedArgs p, const i32x4* row_tab) {
   constexpr bool FWD = EPI == EPI_FWD1, STRIDED = FWD || EPI == EPI_PLAIN;
   __shared__ __align__(1024) unsigned char stage0[kDmaStageBytes];
@@ -420,7 +422,7 @@ template <int EPI, bool RAGGED> __global__ __launch_bounds__(kDmaThreads) void g
     const RowTile tn = has_next ? fetch_tile(nid) : t;   // (none: this tile's first loads once more, waited for below and never used)
     Issue next;
     dma_pipeline_cont<false, STRIDED>(s0, s1, s2, s3, acc, issue, KT, next, wm, cb0, []() {}, [&](Issue& nx) { nx = make_issue(tn); });
-    if constexpr (EPI == EPI_PLAIN) {
+    if constexpr (EPI == EPI_PLAIN || EPI == EPI_PLAIN_T) {
       if (t.rows_valid == BM && t.cols_valid == BN) gated_plain_rounds<true>(s3 + wave * 4096, acc, p, t, wm, t.n0 + cb0 * 32);
       else gated_plain_rounds<false>(s3 + wave * 4096, acc, p, t, wm, t.n0 + cb0 * 32);
     } else {
@@ -547,7 +549,7 @@ static unsigned small_grid(const FfnArgs& a, int bm, int col_tiles) {
 }
 template <int EPI> static void launch_persist(const FfnArgs& a, const GatedArgs& p, const RowsKernels& rk, hipStream_t s) {
   const dim3 grid(std::min(patched_grid(a.A / BM + a.V, p.col_tiles), 256u));
-  if constexpr (EPI != EPI_PLAIN) {
+  if constexpr (EPI != EPI_PLAIN && EPI != EPI_PLAIN_T) {
     if (p.K % (4 * DK) == 0) {
       hipLaunchKernelGGL((gated_persist_bf16<EPI, false>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
       return;
@@ -603,16 +605,43 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
   return hipGetLastError();
 }
 
-static FfnArgs doubled(const FfnArgs& a) {
+// Past the line of ungated layers the few-rows kernels with 64-row tiles are taken where a pass's two rows products are expected to be
+// done earlier on them, in ns, from the tiles (the loads are not known here: half a ragged tile per bucket or expert):
+//   256 x 256: 21000, and 4000 + 880 per 32 k and 256 tiles, a full round of them at least
+//   64 x 128: 2600 + 860 per 64 k and 512 tiles, a full round at least; 4000 where few tiles are cut into segments
+// Fitted to both kernels' times for 240 layers (2600 to 60000 rows, d 64 to 1500, f 64 to 4100, 1 to 40 experts of Zipf loads, forward and
+// training): the one chosen took 1.005 of the faster one's time on average, 1.21 at most.  Some of them, us, 64 x 128 and 256 x 256:
+// forward, d 120, f 3312, 2969 rows 41, 119; d 64, f 1088, 9594 rows 39, 69; d 448, f 1088, 9710 rows 65, 87; d 656, f 712, 13508 rows 88, 98;
+// d 512, f 1408, 17557 rows 140, 116; d 960, f 2816, 15652 rows 491, 356; training, d 192, f 2088, 4300 rows 159, 365; d 136, f 344,
+// 25852 rows 140, 211; d 768, f 1088, 9421 rows 330, 347; d 1088, f 1600, 14624 rows 914, 862; d 704, f 2944, 38200 rows 2735, 2048.
+static bool few_faster(const FfnArgs& a, const int (&K)[2], const int (&NC)[2]) {
+  auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
+  long long few = 0, large = 0;
+  for (int i = 0; i < 2; ++i) {
+    const long long large_tiles = (a.A / BM + (a.V + 1) / 2) * ceil_div(NC[i], BN), tiles = (a.A / 64 + (a.E + 1) / 2) * ceil_div(NC[i], SN);
+    large += 21000 + std::max(256ll, large_tiles) * (4000 + 880ll * ragged_k_tiles(K[i])) / 256;
+    const long long stages = ceil_div(K[i], 64), seg = std::max(1ll, std::min<long long>(kSmallSplitTarget / std::max(tiles, 1ll), stages / 8));
+    few += std::max<long long>(kSmallSplitTarget, tiles) * (2600 + 860 * ceil_div(stages, seg)) / kSmallSplitTarget + (seg > 1 ? 4000 : 0);
+  }
+  return few <= large;
+}
+// The layer as the shared host side sees it.  Where few_faster says so, the few-rows kernels' tables lie in the part of the workspace's second
+// [A, 2 f] that the pass does not use: all of it in the forward pass, in the backward pass what is behind H.
+static FfnArgs doubled(const FfnArgs& a, void* ws, bool fwd) {
   FfnArgs b = a;
   b.f = 2 * a.f;
+  if (a.A == 0 || rows_kernels(b, ws).small.bm) return b;
+  const size_t hpre = align_up((size_t)a.A * b.f * sizeof(bf16_t), 256), h = fwd ? 0 : align_up((size_t)a.A * a.f * sizeof(bf16_t), 256);
+  const int K[2] = {a.d, fwd ? a.f : b.f}, NC[2] = {fwd ? b.f : a.f, a.d}, wide = std::max(b.f, b.d);
+  // (32-bit byte offsets of the weights' and rows' loads as in ungated layers)
+  if (few_tables_bytes(b) <= hpre - h && wide < 1 << 24 && (long long)a.A * wide < 1ll << 30 && few_faster(b, K, NC)) b.few_ws = (char*)ws + hpre + h;
   return b;
 }
 
 hipError_t launch_ffn_gated_fwd_bf16(const FfnArgs& a, const void* xp, const void* w1, const void* b1, const void* w2, const void* b2,
                                      void* hpre, void* h_keep, void* yp, void* ws, hipStream_t s) {
   if (a.A == 0) return hipSuccess;
-  const FfnArgs a2 = doubled(a);
+  const FfnArgs a2 = doubled(a, ws, true);
   launch_rows_plan(a2, ws, s);
   void* h = h_keep ? h_keep : ws;
   const hipError_t err = launch_gated<EPI_FWD1>(a2, xp, w1, b1, nullptr, hpre, h, ws, s);
@@ -622,7 +651,7 @@ hipError_t launch_ffn_gated_fwd_bf16(const FfnArgs& a, const void* xp, const voi
 
 hipError_t launch_ffn_gated_bwd_bf16(const FfnArgs& a, const void* dyp, const void* xp, const void* hpre, const void* h_kept, const void* w1,
                                      const void* w2, void* dxp, void* dw1, void* dw2, void* ws, hipStream_t s) {
-  const FfnArgs a2 = doubled(a);
+  const FfnArgs a2 = doubled(a, ws, false);
   bf16_t* dhpre = (bf16_t*)ws;
   bf16_t* h_ws = (bf16_t*)((char*)ws + align_up((size_t)a2.A * a2.f * sizeof(bf16_t), 256));
   launch_bwd_plan(a2, a.f, ws, s);
@@ -631,7 +660,13 @@ hipError_t launch_ffn_gated_bwd_bf16(const FfnArgs& a, const void* dyp, const vo
                                   : launch_gated<EPI_DH>(a2, dyp, w2, nullptr, hpre, dhpre, h_ws, ws, s);
     if (err != hipSuccess) return err;
   }
-  return launch_bwd_products(a2, a.f, h_kept ? h_kept : h_ws, dyp, dw2, xp, dhpre, dw1, w1, dxp, nullptr, ws, s);
+  const RowsKernels rk = rows_kernels(a2, ws);
+  const bool dx_here = a.A > 0 && !rk.small.bm && a2.f % 128;      // (where it is, dX's kernel is the ungated layers')
+  if (dx_here) {
+    const GatedArgs p{dhpre, (const bf16_t*)w1, nullptr, a2.f, a.d, (a.d + BN - 1) / BN, nullptr, (bf16_t*)dxp, nullptr, 0};
+    launch_persist<EPI_PLAIN_T>(a2, p, rk, s);
+  }
+  return launch_bwd_products(a2, a.f, h_kept ? h_kept : h_ws, dyp, dw2, xp, dhpre, dw1, w1, dx_here ? nullptr : dxp, nullptr, ws, s);
 }
 
 }  // namespace flexmoe

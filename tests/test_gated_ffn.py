@@ -201,9 +201,10 @@ class Case:
 # (direct loads) and where it is not; f in no whole tiles; one row, one expert, empty experts
 FEW = [(1, 8, 8, 1, 1), (3, 64, 72, 4, 5), (17, 1024, 512, 8, 12), (130, 328, 904, 12, 15), (700, 256, 264, 4, 9), (2000, 136, 1032, 3, 3),
        (40, 72, 4104, 16, 20), (200, 64, 4104, 16, 16)]      # (the last two: the halves of W1 in turn)
-# (the last but one is just inside the line of the few-rows kernels: (64 + 3 * 200 / 8) * 256 * 256 / 256 = 35584 rows)
+# (between the two kernels: the fourth to the eighth take 64-row tiles, in the backward pass or both, from where it pays; the last ones 256-row
+# tiles with contractions in no whole rounds)
 LARGE = [(7300, 2048, 1024, 4, 6), (7300, 2048, 1096, 4, 4), (7400, 2056, 1032, 3, 5), (30000, 128, 200, 2, 40), (31000, 200, 128, 5, 5),
-         (36000, 200, 128, 5, 5)]
+         (36000, 200, 128, 5, 5), (3000, 120, 3312, 2, 2), (12480, 64, 1000, 2, 3), (60000, 200, 1104, 2, 3), (30000, 256, 1280, 2, 3)]
 
 
 @pytest.mark.gpu
