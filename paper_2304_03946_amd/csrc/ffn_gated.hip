@@ -20,7 +20,7 @@
 //
 // What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.  Measured:
 // 32768 tokens x 2, d 2048, f 5632, 32 experts: first product 2.86 ms (1.06 PFLOP/s), Y 1.25 (1.21), dH 1.75 (0.87), dX 2.68 (1.13), both weight
-// gradients 4.43 (1.02); a large library product runs at 1.42.  16 tokens x 2, d 1024, f 4096, 17 experts with rows: 427 MB of weights in 89 us.
+// gradients 4.43 (1.02); a large library product runs at 1.42.  16 tokens x 2, d 1024, f 4096, 17 experts with rows on average: 427 MB of weights in 89 - 105 us.
 #include <algorithm>
 
 #include "common.h"

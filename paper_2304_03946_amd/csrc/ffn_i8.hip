@@ -13,7 +13,7 @@
 // 6 bytes per element (bf16): 0.21 of 2.53 ms at 32768 tokens x 2, d 2048, f 5632.
 //
 // What bounds them: the matrix cores at hundreds of rows per expert (there, gated, both products 2.0 Pop/s; a large library product reaches
-// 2.47), the weights' bytes at few (48 tokens x 2, d 2048, f 4096, 64 experts: 1.0 GB in 213 us), launches and first loads between (one token
+// 2.47), the weights' bytes at few (48 tokens x 2, d 2048, f 4096, 64 experts: 1.0 GB in 213 - 226 us), launches and first loads between (one token
 // x 2, d 1024, f 4096: 4.0, 11.9, 4.0 and 7.7 us).
 #include <algorithm>
 
