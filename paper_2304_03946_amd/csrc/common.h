@@ -71,6 +71,9 @@ __device__ __forceinline__ float act_apply(float z, int act) {
   const float c = 0.79788456080286536f;
   return 0.5f * z * (1.f + tanhf(c * (z + 0.044715f * z * z * z)));
 }
+// GELU_TANH': from |z| = 16 on 1 - tanh^2 is 0, and the polynomial it is multiplied by is held there: from 5e19 on it would be infinite, and
+// their product no number.
+constexpr float kTanhSlopeMax = 16.f;
 __device__ __forceinline__ float act_deriv(float z, int act) {
   if (act == FLEXMOE_RELU) return z > 0.f ? 1.f : 0.f;
   if (act == FLEXMOE_GELU_ERF)
@@ -78,7 +81,8 @@ __device__ __forceinline__ float act_deriv(float z, int act) {
   const float c = 0.79788456080286536f;
   float u = c * (z + 0.044715f * z * z * z);
   float th = tanhf(u);
-  return 0.5f * (1.f + th) + 0.5f * z * (1.f - th * th) * c * (1.f + 3.f * 0.044715f * z * z);
+  const float zc = fminf(fmaxf(z, -kTanhSlopeMax), kTanhSlopeMax);
+  return 0.5f * (1.f + th) + 0.5f * z * (1.f - th * th) * c * (1.f + 3.f * 0.044715f * zc * zc);
 }
 
 // Fast forms for the bf16 GEMM epilogues, where results are rounded to bf16 (relative 2^-9).
@@ -117,7 +121,8 @@ template <int ACT> __device__ __forceinline__ void act_both(float z, float* a, f
     const float c = 0.79788456080286536f;
     const float th = fast_tanh(c * fmaf(0.044715f * z, z * z, z));
     *a = 0.5f * z * (1.f + th);
-    *da = 0.5f * (1.f + th) + 0.5f * z * (1.f - th * th) * c * fmaf(3.f * 0.044715f * z, z, 1.f);
+    const float zc = __builtin_amdgcn_fmed3f(z, -kTanhSlopeMax, kTanhSlopeMax);
+    *da = 0.5f * (1.f + th) + 0.5f * z * (1.f - th * th) * c * fmaf(3.f * 0.044715f * zc, zc, 1.f);
   }
 }
 template <int ACT> __device__ __forceinline__ float act_fast(float z) {

@@ -1,0 +1,86 @@
+"""Experts at the ends of the number range, against the formulas in 64 bits.
+
+Where act'(z) is 0 or 1 to more places than its type has (|z| >= 30 in every activation but SiLU), dHpre is a product of dH that carries
+fp32 sums of d terms (2^-23 sqrt(d) of the root of the sum of their squares, six standard deviations of errors uniform in that: `sums`) and
+one rounding per factor and for the type, u = finfo(t).eps / 2.
+"""
+import pytest
+import torch
+
+from test_gated_ffn import SPREAD, Case, decode, dot, float32_by_default, sums  # noqa: F401
+
+LARGE = (1e19, -1e19, 6e19, -6e19, 1e25, -1e25, 1e33, -1e33, 30.0, -30.0)
+
+
+def _b():
+    from paper_2304_03946_amd import binding as B
+    B.load_library()
+    return B
+
+
+def d_hidden(c, rows, dt):
+    """dH = dY W2^T and its noise."""
+    dh, noise = (torch.zeros(c.A, c.f, dtype=torch.float64, device="cuda") for _ in range(2))
+    for e in range(c.E):
+        r = torch.nonzero(rows == e).flatten()
+        w2t = c.w2[e].double().T.contiguous()
+        dh[r] = c.dy[r].double() @ w2t
+        noise[r] = SPREAD * sums(c.d) * dot(c.dy[r].double(), w2t)
+    return dh, noise
+
+
+# rows, d, f: few rows; 256 x 256 tiles, contractions in whole rounds of 128 and not
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu_erf", "gelu_tanh"])
+@pytest.mark.parametrize("A,d,f", [(40, 64, 72), (7300, 2048, 1024), (7400, 2056, 1032)])
+def test_slopes_of_gates_far_from_zero(A, d, f, act, dtype):
+    if dtype == "f32" and A > 1000:
+        A, d, f = 1600, 136, 264
+    c = Case(A, d, f, 2, 3, dtype, act, True, seed=7)
+    far = torch.arange(f, device="cuda") % 3 != 0
+    gate = torch.tensor(LARGE, device="cuda")[torch.arange(f, device="cuda") % len(LARGE)]
+    c.b1[:, :f] = torch.where(far, gate, torch.zeros_like(gate)).to(c.dt)
+    c.w1[:, :, :f][:, :, far] = 0
+    c.fwd()
+    g, up = decode(c.hpre)[:, :f], decode(c.hpre)[:, f:]
+    assert torch.isfinite(c.y).all() and (g[:, far].abs() >= 29).all()
+    dh, noise = d_hidden(c, c.rows, c.dt)
+    u = c.u()
+    for kept in (True, False):
+        c.bwd(kept)
+        got = c.ws[:A * 2 * f * c.dxp.element_size()].view(c.dt).view(A, 2 * f).double()
+        for t in (got, c.dxp, c.dw1, c.dw2):
+            assert torch.isfinite(t).all()
+        slope = (g > 0).double()
+        for name, v, want, n in (("dG", got[:, :f], dh * up * slope, noise * up.abs() * slope),
+                                 ("dU", got[:, f:], dh * g * slope, noise * g.abs() * slope)):
+            tol = (u + 2.0 ** -21) * want.abs() + (1 + u) * n + 1e-37
+            if act != "relu":                     # at |z| = 30 the lower tail is below 1e-12 of |z|; the fp32 forms' sums cancel to 2^-22
+                tol = tol + 2.0 ** -22 * dh.abs() * (up.abs() if name == "dG" else g.abs().clamp(max=30))
+            worst = float(((v - want).abs() / tol)[:, far].max())
+            assert worst <= 1 + 2 * u, (name, kept, worst)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,A,d,f", [("bf16", 40, 64, 72), ("bf16", 40, 128, 72), ("bf16", 7400, 2056, 1032), ("bf16", 7300, 2048, 1024),
+                                         ("f32", 40, 64, 72), ("f32", 1600, 136, 264)])
+@pytest.mark.parametrize("act", ["relu", "gelu_erf", "gelu_tanh"])
+def test_slopes_far_from_zero_without_a_gate(dtype, A, d, f, act):
+    """The same for ungated layers: GELU from its table (d a multiple of 128), evaluated, and in fp32."""
+    B = _b()
+    c = Case(A, d, f, 2, 3, dtype, act, False, seed=8)
+    hpre = torch.tensor(LARGE, device="cuda").to(c.dt)[torch.arange(A * f, device="cuda") % len(LARGE)].view(A, f).clone()
+    w1 = c.w1[:, :, :f].contiguous()
+    dw1 = torch.empty_like(w1)
+    dh, noise = d_hidden(c, c.rows, c.dt)
+    u = c.u()
+    ws = torch.empty(B.flexmoe_workspace_bytes(A, d, f, 2, 1, 3, B.BF16 if dtype == "bf16" else B.F32), dtype=torch.uint8, device="cuda")
+    B.flexmoe_expert_ffn_bwd(c.dy, c.x, hpre, w1, c.w2, c.voff, c.owner, c.code, c.dxp, dw1, c.dw2, ws)
+    got = ws[:A * f * c.dxp.element_size()].view(c.dt).view(A, f).double()
+    for t in (got, c.dxp, dw1, c.dw2):
+        assert torch.isfinite(t).all()
+    slope = (hpre > 0).double()
+    tol = (u + 2.0 ** -21) * (dh * slope).abs() + (1 + u) * noise * slope + 2.0 ** -22 * dh.abs() + 1e-37
+    worst = float(((got - dh * slope).abs() / tol).max())
+    assert worst <= 1 + 2 * u, worst
