@@ -337,8 +337,8 @@ __global__ __launch_bounds__(kF32Threads, 2) void rows_gemm_f32(const float* __r
 
 // The two products of gated experts that have an activation (H = act(G) * U; G, U, dG and dU are the halves of Hpre and dHpre [A, 2 f]).
 // EPI_FWD1: [G, U] = In . W1_e + b1_e, W1_e [K, 2 f]; a tile's 64 columns are 32 of G and the same 32 of U, 16 and 16 in turn, so that a
-// wave's blocks j = 0 and 1 are G and U of the same outputs.  EPI_DH: dH = In . W2_e^T, W2_e [f, K], in 64 columns; dG = dH * U * act'(G),
-// dU = dH * act(G).
+// wave's blocks j = 0 and 1 are G and U of the same outputs.  EPI_DH: dH = In . W2_e^T, W2_e [f, K], in 64 columns; dG = dH * act'(G) * U (in
+// this order: dH * U may overflow where a closed gate makes dG small), dU = dH * act(G).
 __device__ __forceinline__ void gate_f32(float z, int act, float* a, float* da) {
   if (act == FLEXMOE_SILU) {
     const float s = 1.f / (1.f + expf(-z));
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kF32Threads, 2) void rows_gated_f32(const float* __
         const float dh = acc[x >> 1][x & 1][q];
         float a, da;
         gate_f32(zg[x][q], act, &a, &da);
-        dg[q] = dh * zu[x][q] * da;
+        dg[q] = dh * da * zu[x][q];
         du[q] = dh * a;
         h[q] = a * zu[x][q];
       }

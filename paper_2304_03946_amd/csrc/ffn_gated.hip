@@ -5,6 +5,7 @@
 // and for an upstream gradient dY
 //   dH = dY W2^T;   dG = dH * U * act'(G),  dU = dH * act(G)      the epilogue of dH's product; dHpre = [dG, dU]
 //   dX = dHpre W1^T,  dW1 = X^T dHpre,  dW2 = H^T dY
+// (dG as (dH act'(G)) U: |act'| < 1.13, so what overflows is the product itself; dH U would where a closed gate makes it small or zero)
 //
 // The products without an activation -- Y, dX, dW1, dW2 -- are those of an ungated layer with 2 f (W1) or f (W2) columns in the middle,
 // on the kernels of ffn_bf16.hip.  The two with one have kernels here, on the same loops:
@@ -279,7 +280,7 @@ __device__ __forceinline__ void gated_dh_rounds(float* patch, int jh, const DmaA
       for (int q = 0; q < 4; ++q) {
         float a, da;
         gate_act<ACT>(g[q], &a, &da);
-        dg[q] = dh[q] * u[q] * da;
+        dg[q] = dh[q] * da * u[q];
         du[q] = dh[q] * a;
         h[q] = a * u[q];
       }
@@ -489,7 +490,7 @@ template <int BM, int EPI, int GATE> struct GatedSmallPol {
             const float dh = acc[0][i][j][q];
             float a, da;
             gate_act<ACT>(g[q], &a, &da);
-            dg[q] = dh * u[q] * da;
+            dg[q] = dh * da * u[q];
             du[q] = dh * a;
             h[q] = a * u[q];
           }

@@ -7,7 +7,7 @@ one rounding per factor and for the type, u = finfo(t).eps / 2.
 import pytest
 import torch
 
-from test_gated_ffn import SPREAD, Case, decode, dot, float32_by_default, sums  # noqa: F401
+from test_gated_ffn import SPREAD, Case, act64, decode, dot, float32_by_default, sums  # noqa: F401
 
 LARGE = (1e19, -1e19, 6e19, -6e19, 1e25, -1e25, 1e33, -1e33, 30.0, -30.0)
 
@@ -84,3 +84,35 @@ def test_slopes_far_from_zero_without_a_gate(dtype, A, d, f, act):
     tol = (u + 2.0 ** -21) * (dh * slope).abs() + (1 + u) * noise * slope + 2.0 ** -22 * dh.abs() + 1e-37
     worst = float(((got - dh * slope).abs() / tol).max())
     assert worst <= 1 + 2 * u, worst
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu_erf"])
+@pytest.mark.parametrize("A,d,f", [(40, 64, 72), (7300, 2048, 1024), (7400, 2056, 1032)])
+def test_closed_gates_keep_large_factors_out(A, d, f, act, dtype):
+    """dG = dH U act'(G) where dH U is beyond fp32 and act'(G) next to nothing: the product fits, or is zero."""
+    if dtype == "f32" and A > 1000:
+        A, d, f = 1600, 136, 264
+    c = Case(A, d, f, 2, 3, dtype, act, True, seed=6)
+    c.w1.zero_()
+    c.b1[:, :f] = -60.0 if act == "silu" else -8.0
+    c.b1[:, f:] = 1e25
+    c.dy *= 1e20
+    c.fwd()
+    dh, noise = d_hidden(c, c.rows, c.dt)
+    assert float(dh.abs().max()) * 1e25 > 3.5e38
+    g, up = decode(c.hpre)[:, :f], decode(c.hpre)[:, f:]
+    slope = act64(act, g)[1]
+    want = dh * up * slope
+    for kept in (True, False):
+        c.bwd(kept)
+        dz = c.ws[:A * 2 * f * c.dxp.element_size()].view(c.dt).view(A, 2 * f)
+        for t in (dz, c.dxp, c.dw1, c.dw2):
+            assert torch.isfinite(t).all()
+        if act == "relu":
+            assert not dz.any() and not c.dxp.any() and not c.dw1.any() and not c.dw2.any()
+        if act == "silu":                         # one rounding of z / ln 2 in the exponent: 2^-24 of 87, and as much for the constant
+            u = c.u()
+            tol = (u + 2.0 ** -15) * want.abs() + (1 + u) * noise * (up * slope).abs()
+            assert float(((dz[:, :f].double() - want).abs() / tol).max()) <= 1 + 2 * u
