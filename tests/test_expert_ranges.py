@@ -1,14 +1,17 @@
-"""Experts at the ends of the number range, against the formulas in 64 bits.
+"""Gated and 8-bit experts at the ends of the number range, against the formulas in 64 bits.
 
 Where act'(z) is 0 or 1 to more places than its type has (|z| >= 30 in every activation but SiLU), dHpre is a product of dH that carries
 fp32 sums of d terms (2^-23 sqrt(d) of the root of the sum of their squares, six standard deviations of errors uniform in that: `sums`) and
 one rounding per factor and for the type, u = finfo(t).eps / 2.
 """
+import math
+
 import pytest
 import torch
 
 from test_gated_ffn import SPREAD, Case, act64, decode, dot, float32_by_default, sums  # noqa: F401
 
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 LARGE = (1e19, -1e19, 6e19, -6e19, 1e25, -1e25, 1e33, -1e33, 30.0, -30.0)
 
 
@@ -116,3 +119,38 @@ def test_closed_gates_keep_large_factors_out(A, d, f, act, dtype):
             u = c.u()
             tol = (u + 2.0 ** -15) * want.abs() + (1 + u) * noise * (up * slope).abs()
             assert float(((dz[:, :f].double() - want).abs() / tol).max()) <= 1 + 2 * u
+
+
+def hidden_alone(z, act, gated, dtype):
+    """H = act(z) (times 1) of 8-bit experts, one expert for each z, read from the scales: x = 0, so the pre-activations are the biases, all
+    of a row's H are equal, its integers are 127 and y is 127 times their scale."""
+    B = _b()
+    E, d, f = len(z), 16, 16
+    cols = 2 * f if gated else f
+    b1 = torch.ones(E, cols, device="cuda")
+    b1[:, :f] = z[:, None]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    w2 = torch.zeros(E, d, f, dtype=torch.int8, device="cuda")
+    w2[:, :, 0] = 1
+    y = torch.empty(E, d, dtype=DT[dtype], device="cuda")
+    ws = torch.empty(B.flexmoe_i8_workspace_bytes(E, d, f, E, 1, E, int(gated)), dtype=torch.uint8, device="cuda")
+    code = dict(relu=B.RELU, gelu_erf=B.GELU_ERF, gelu_tanh=B.GELU_TANH, silu=B.SILU)[act]
+    B.flexmoe_expert_ffn_i8_fwd(torch.zeros(E, d, device="cuda", dtype=DT[dtype]), torch.arange(E, **i32), 1, torch.arange(E + 1, **i32),
+                                torch.arange(E, **i32), torch.zeros(E, cols, d, dtype=torch.int8, device="cuda"), torch.ones(E, cols, device="cuda"),
+                                b1.to(DT[dtype]), w2, torch.ones(E, d, device="cuda"), None, gated, code, y, ws)
+    assert torch.equal(y, y[:, :1].expand(E, d))
+    return y[:, 0].double()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("act", ["relu", "gelu_erf", "gelu_tanh", "silu"])
+def test_fp32_activations_of_8_bit_experts(act, gated):
+    """H of fp32 layers is what the other fp32 layers make: SiLU to 2^-21 of its value (an exponential within 2^-23, and five roundings of
+    2^-24: the sum, the quotient, the product, H / 127 and 127 times that), GELU to 2^-22 |z| (an error function or tanh within 2^-23, halved, next to 1)."""
+    z = torch.cat([-torch.logspace(-3, math.log10(80), 100), torch.logspace(-3, 2, 100)]).float().cuda()
+    want = act64(act, z.double())[0]
+    got = hidden_alone(z, act, gated, "f32")
+    tol = 2.0 ** -21 * want.abs() + (2.0 ** -22 * z.double().abs() if act.startswith("gelu") else 0) + 1e-43
+    worst = (got - want).abs() / tol
+    assert float(worst.max()) <= 1, (float(z[worst.argmax()]), float(worst.max()))
