@@ -204,7 +204,8 @@ int flexmoe_quantize_rows(const void* x, int M, int K, int dtype, void* q, float
 int flexmoe_quantize_weights(const void* w, int E, int K, int NC, int dtype, void* q, float* scale, void* stream);
 
 /* Bytes of scratch for flexmoe_expert_ffn_i8_fwd of these sizes and for flexmoe_expert_matmul_i8 of any K and NC with these N, E, k, V; 0 for
-   sizes that neither takes (the product of d and f serves any f that is a multiple of 8).  Never falls where N alone grows. */
+   sizes that neither takes (the product has d as K and f, gated 2f, as NC: any multiple of 8 below 2^20).  Never falls where N alone grows.
+   Good for either dtype: H [N*k,f] has room for four bytes an element. */
 size_t flexmoe_i8_workspace_bytes(int N, int d, int f, int E, int k, int V, int gated);
 
 /*

@@ -274,8 +274,8 @@ static bool i8_counts_ok(int N, int k, int E, int V) {
 }
 
 size_t flexmoe_i8_workspace_bytes(int N, int d, int f, int E, int k, int V, int gated) {
-  if (!i8_counts_ok(N, k, E, V) || f >= (1 << 17) || !i8_dims_ok(d, gated ? 2ll * f : f, 8)) return 0;      // (f as a product's columns)
-  return i8_ws_bytes(N, d, f, N * k, E, V, true);
+  if (!i8_counts_ok(N, k, E, V) || !i8_dims_ok(d, gated ? 2ll * f : f, 8)) return 0;
+  return i8_ws_bytes(N, d, f, N * k, E, V, i8_dims_ok(f, d, 16));      // (else only as a product's columns: more than a contraction has, or no multiple of 16)
 }
 
 int flexmoe_quantize_rows(const void* x, int M, int K, int dtype, void* q, float* scale, void* stream) {
