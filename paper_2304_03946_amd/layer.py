@@ -37,9 +37,16 @@ class QuantizedExperts:
     (gated: [E, d, 2 f]) and w2 [E, f, d]; the biases stay as they are."""
 
     def __init__(self, w1, w2, b1=None, b2=None):
+        E, f, d = w2.shape
+        cols = w1.shape[-1]
+        if tuple(w1.shape) != (E, d, cols) or cols not in (f, 2 * f):
+            raise ValueError(f"w1 {tuple(w1.shape)} is neither [E, d, f] nor [E, d, 2 f] for w2 [E, f, d] = {tuple(w2.shape)}")
+        for b, n in ((b1, cols), (b2, d)):
+            if b is not None and tuple(b.shape) != (E, n):
+                raise ValueError(f"a bias of shape {tuple(b.shape)} where [{E}, {n}] belongs")
+        self.sizes, self.gated = (E, d, f), cols == 2 * f
         self.b1, self.b2 = b1, b2
         (self.w1, self.s1), (self.w2, self.s2) = self._quantize(w1), self._quantize(w2)
-        self.gated = w1.shape[2] == 2 * w2.shape[1]
 
     @staticmethod
     def _quantize(w):
@@ -195,6 +202,10 @@ class MoELayer:
         neither xp nor hpre is written."""
         if experts.gated != self.gated:
             raise ValueError("the experts were made for a layer of the other kind (gated or not)")
+        if experts.sizes != (self.E, self.d, self.f):
+            raise ValueError(f"experts of [E, d, f] = {experts.sizes} in a layer of {(self.E, self.d, self.f)}")
+        if any(b is not None and b.dtype != self.y.dtype for b in (experts.b1, experts.b2)):
+            raise ValueError("the experts' biases have another type than the layer")
         if not hasattr(self, "ws_i8"):
             nbytes = B.flexmoe_i8_workspace_bytes(self.N, self.d, self.f, self.E, self.k, self.V, int(self.gated))
             if nbytes == 0:

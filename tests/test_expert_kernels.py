@@ -56,3 +56,22 @@ def test_wide_product(N, dtype):
     work = torch.empty(_b().flexmoe_i8_workspace_bytes(N, K, NC, E, k, V, 0), dtype=torch.uint8, device="cuda")
     _b().flexmoe_expert_matmul_i8(q, s, t.src, k, t.voff, t.owner, wq, ws, bias, y, work)
     check_product(y, q, s, wq, ws, bias, t.token, t.expert, dtype)
+
+
+# ---- the layer's checks ------------------------------------------------------------------------------
+def test_experts_that_do_not_fit():
+    """Shapes that the kernels would take at their word (they get E, d and f from one of the tensors) are refused on the host."""
+    from types import SimpleNamespace
+    from paper_2304_03946_amd import layer as L
+    B = _b()
+    new = torch.zeros
+    for w1, w2, b1, b2 in (((2, 16, 48), (2, 32, 16), None, None), ((3, 16, 32), (2, 32, 16), None, None), ((2, 32, 32), (2, 32, 16), None, None),
+                           ((2, 16, 96), (2, 32, 16), None, None), ((2, 16, 64), (2, 32, 16), (2, 32), None), ((2, 16, 32), (2, 32, 16), (2, 64), None),
+                           ((2, 16, 32), (2, 32, 16), None, (2, 32)), ((2, 16, 32), (2, 32, 16), None, (1, 16))):
+        with pytest.raises(ValueError):
+            L.QuantizedExperts(new(w1), new(w2), None if b1 is None else new(b1), None if b2 is None else new(b2))
+    m = L.MoELayer(4, 16, 32, 2, 1, 2, B.BF16, B.RELU, device="cpu")
+    fits = dict(sizes=(2, 16, 32), gated=False, b1=None, b2=None)
+    for wrong in (dict(sizes=(1, 16, 32)), dict(sizes=(2, 32, 32)), dict(sizes=(2, 16, 16)), dict(gated=True), dict(b1=new(2, 32)), dict(b2=new(2, 16))):
+        with pytest.raises(ValueError):
+            m.forward_i8(new(4, 16), new(16, 2), SimpleNamespace(**{**fits, **wrong}), [0, 1, 2], [0, 1])
