@@ -558,6 +558,20 @@ template <int EPI> static void launch_persist(const FfnArgs& a, const GatedArgs&
   }
   hipLaunchKernelGGL((gated_persist_bf16<EPI, true>), grid, dim3(kDmaThreads), 0, s, p, (const i32x4*)rk.row_tab);
 }
+// (a: planned as a layer with a.f = 2 f, rows_kernels)
+static SmallCore gated_out_core(const FfnArgs& a, const RowsKernels& rk, const bf16_t* in, const bf16_t* w) {
+  return SmallCore{in, w, rk.small.tab, rk.small.rowmap, a.f / 2, a.d, (a.d + SN - 1) / SN, rk.small.rowmap, rk.small_partial, rk.small.counters,
+                   rk.small_slots, a.A};
+}
+// The first product (fwd) or dH's.  turns: the halves of W1 in turn, where that leaves a tile for every workgroup (a row tile per expert that can
+// have rows), else mixed.
+static SmallCore gated_core(const FfnArgs& a, const RowsKernels& rk, bool fwd, const bf16_t* in, const bf16_t* w, bool* turns) {
+  const int f = a.f / 2;
+  *turns = fwd && (long long)std::min(a.A, a.E) * ((f + SN - 1) / SN) >= kSmallSplitTarget;
+  const int cols = fwd && !*turns ? SN / 2 : SN;
+  return SmallCore{in, w, rk.small.tab, rk.small.rowmap, a.d, fwd ? 2 * f : f, (f + cols - 1) / cols, rk.small.rowmap, rk.small_partial,
+                   rk.small.counters, rk.small_slots, a.A};
+}
 static hipError_t launch_gated_out(const FfnArgs& a, const void* h, const void* w2, const void* b2, void* yp, void* ws, hipStream_t s) {
   const int f = a.f / 2;
   const RowsKernels rk = rows_kernels(a, ws);
@@ -567,14 +581,12 @@ static hipError_t launch_gated_out(const FfnArgs& a, const void* h, const void* 
     launch_persist<EPI_PLAIN>(a, p, rk, s);
     return hipGetLastError();
   }
-  const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, f, a.d, (a.d + SN - 1) / SN, rk.small.rowmap, rk.small_partial, rk.small.counters,
-                    rk.small_slots, a.A};
+  const SmallCore c = gated_out_core(a, rk, p.in, p.w);
   const dim3 grid(small_grid(a, rk.small.bm, c.col_tiles));
   if (rk.small.bm == 32) hipLaunchKernelGGL(gated_out_small_bf16<32>, grid, dim3(kSmallThreads), 0, s, c, p);
   else hipLaunchKernelGGL(gated_out_small_bf16<64>, grid, dim3(kSmallThreads), 0, s, c, p);
   return hipGetLastError();
 }
-// a: planned as a layer with a.f = 2 f (rows_kernels)
 template <int EPI>
 static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, const void* bias, const void* hpre_in, void* out0, void* out1,
                                void* ws, hipStream_t s) {
@@ -584,11 +596,8 @@ static hipError_t launch_gated(const FfnArgs& a, const void* in, const void* w, 
   const GatedArgs p{(const bf16_t*)in, (const bf16_t*)w, (const bf16_t*)bias, K, f, FWD ? (f + GN - 1) / GN : (f + BN - 1) / BN,
                     (const bf16_t*)hpre_in, (bf16_t*)out0, (bf16_t*)out1, a.act};
   if (rk.small.bm) {
-    // the halves in turn where that leaves a tile for every workgroup (a row tile per expert that can have rows), else mixed
-    const bool turns = FWD && (long long)std::min(a.A, a.E) * ((f + SN - 1) / SN) >= kSmallSplitTarget;
-    const int cols = FWD && !turns ? SN / 2 : SN;
-    const SmallCore c{p.in, p.w, rk.small.tab, rk.small.rowmap, K, FWD ? 2 * f : f, (f + cols - 1) / cols, rk.small.rowmap, rk.small_partial,
-                      rk.small.counters, rk.small_slots, a.A};
+    bool turns;
+    const SmallCore c = gated_core(a, rk, FWD, p.in, p.w, &turns);
     const dim3 grid(small_grid(a, rk.small.bm, c.col_tiles));
     constexpr int kGate = FWD ? GATE_MIXED : GATE_NONE;
     if constexpr (FWD) {
@@ -671,3 +680,22 @@ hipError_t launch_ffn_gated_bwd_bf16(const FfnArgs& a, const void* dyp, const vo
 }
 
 }  // namespace flexmoe
+
+// For tests: which rows kernels a bf16 call of a gated layer takes, with row_tiles row tiles in use.  For the forward pass in out[0 .. 4], for the
+// backward pass in out[5 .. 9]: row tiles of the few-rows kernels (0: the 256 x 256 ones); whether they are taken past the ungated layers' line;
+// the halves of W1 in turn; contraction segments of the product with an activation; of the second product (backward: 0).
+extern "C" void flexmoe_debug_gated_paths(int A, int d, int f, int E, int V, int row_tiles, long long* out) {
+  using namespace flexmoe;
+  const FfnArgs a{A, d, f, E, V, FLEXMOE_SILU, nullptr, nullptr};
+  for (int b = 0; b < 2; ++b, out += 5) {
+    const FfnArgs a2 = doubled(a, nullptr, b == 0);
+    const RowsKernels rk = rows_kernels(a2, nullptr);
+    bool turns;
+    const SmallCore c = gated_core(a2, rk, b == 0, nullptr, nullptr, &turns);
+    out[0] = rk.small.bm;
+    out[1] = a2.few_ws != nullptr;
+    out[2] = rk.small.bm && turns;
+    out[3] = rk.small.bm ? core_segments(c, row_tiles, SK, turns ? 2 : 1) : 0;
+    out[4] = rk.small.bm && b == 0 ? core_segments(gated_out_core(a2, rk, nullptr, nullptr), row_tiles, SK, 1) : 0;
+  }
+}

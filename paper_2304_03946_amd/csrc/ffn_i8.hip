@@ -638,13 +638,15 @@ template <int EPI, typename T, bool GATHER> static void launch_i8_persist(const 
   if (p.K % (4 * DK)) hipLaunchKernelGGL((i8_persist<EPI, T, GATHER, true>), grid, dim3(kDmaThreads), 0, s, p, row_tab);
   else hipLaunchKernelGGL((i8_persist<EPI, T, GATHER, false>), grid, dim3(kDmaThreads), 0, s, p, row_tab);
 }
+static SmallCore i8_core(const FfnArgs& a, const I8Args& p, int bm, int wcols, const I8Ws& w) {
+  const int cols = bm == 64 ? i8_cols<64>() : i8_cols<16>();
+  return SmallCore{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters, kSmallSlots, a.A};
+}
 template <int EPI, typename T>
 static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, hipStream_t s) {
   constexpr bool GATE = EPI == I8_GATE;
   if (bm) {
-    const int wcols = GATE ? 2 * p.NC : p.NC;
-    const int cols = bm == 64 ? i8_cols<64>() : i8_cols<16>();
-    const SmallCore c{p.in, p.w, w.small_tab, w.rowmap, p.K, wcols, (wcols + cols - 1) / cols, p.gsrc ? w.tokmap : w.rowmap, w.partial, w.counters, kSmallSlots, a.A};
+    const SmallCore c = i8_core(a, p, bm, GATE ? 2 * p.NC : p.NC, w);
     const long long most = ((long long)a.A / bm + a.E) * c.col_tiles * kSmallSplitMax;
     const dim3 grid((unsigned)std::min<long long>(kSmallSplitTarget, most));
     if (bm == 16) hipLaunchKernelGGL((i8_small<16, EPI, T>), grid, dim3(kSmallThreads), 0, s, c, p);
@@ -663,7 +665,7 @@ static hipError_t launch_i8(const FfnArgs& a, I8Args p, int bm, const I8Ws& w, h
   return hipGetLastError();
 }
 
-// few: row tiles the plan is for, 0: none
+// bm1, bm2: row tiles of the few-rows kernels that the products take (i8_bm), 0: the 256 x 256 kernel, which looks tiles up in another table
 template <typename T>
 static void launch_prep(const FfnArgs& a, int bm1, int bm2, const int32_t* src, int k, I8Prep g, const I8Ws& w, hipStream_t s) {
   const int bm = bm1 ? bm1 : bm2;
@@ -744,3 +746,17 @@ hipError_t launch_quantize_weights(const void* w, int E, int K, int NC, int dtyp
 }
 
 }  // namespace flexmoe
+
+// For tests: which kernel a product of 8-bit experts takes (wcols: its weight columns, 2 f with a gate), with row_tiles row tiles in use.
+// out[0] row tiles of the few-rows kernel, 0: the 256 x 256 one; [1] that one's form for contractions in no whole rounds; [2] the few-rows
+// kernel's contraction segments.
+extern "C" void flexmoe_debug_i8_paths(int N, int k, int K, int wcols, int E, int V, int gathered, int row_tiles, long long* out) {
+  using namespace flexmoe;
+  const FfnArgs a{N * k, K, wcols, E, V, FLEXMOE_RELU, nullptr, nullptr};
+  I8Args p{};
+  p.K = K / 2;
+  const int bm = i8_bm(a, K, wcols, gathered != 0, N);
+  out[0] = bm;
+  out[1] = !bm && p.K % (4 * DK);
+  out[2] = bm ? core_segments(i8_core(a, p, bm, wcols, I8Ws{}), row_tiles, bm == 64 ? CoreCfg<64, i8_cols<64>()>::kKUnits : CoreCfg<16, i8_cols<16>()>::kKUnits, 1) : 0;
+}

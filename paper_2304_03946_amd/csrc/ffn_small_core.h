@@ -55,7 +55,7 @@ template <int BM, int COLS> struct CoreCfg {
 // least eight: 522 rows of 7 experts (d 408, f 2080) 35.0, 28.6; 4503 of 12 (training) 145.7, 136.4; 600 8-bit rows of 8 experts
 // 21.7, 20.0; few rows per tile: 5 rows of one expert (d 1664, f 1608) 21.6, 26.2; 8 8-bit rows (1696 x 1808) 16.9, 18.2.
 // `tiles` counts partial tiles, of which there is room for `slots`.
-__device__ __forceinline__ int core_segments(int tiles, int k_stages, int row_tiles, int rows, int slots) {
+__host__ __device__ inline int core_segments(int tiles, int k_stages, int row_tiles, int rows, int slots) {
   const int least = rows > 16 * row_tiles ? 2 * kSmallSplitKTiles : kSmallSplitKTiles;
   int s = 1;
   while (s < kSmallSplitMax && tiles * s * 2 <= kSmallSplitTarget && k_stages >= 2 * s * least) s *= 2;
@@ -64,6 +64,10 @@ __device__ __forceinline__ int core_segments(int tiles, int k_stages, int row_ti
   return s;
 }
 enum { GATE_NONE = 0, GATE_MIXED = 1, GATE_TURNS = 2 };
+// The same on the host, for a product with row_tiles row tiles in use and stages of k_units (H: accumulators, see small_core).
+inline int core_segments(const SmallCore& c, int row_tiles, int k_units, int H) {
+  return core_segments(row_tiles * c.col_tiles * H, (c.K + k_units - 1) / k_units, row_tiles, c.rows, c.slots);
+}
 
 template <int BM, int COLS, bool WT, int GATE, typename V4, typename Pol>
 __device__ __forceinline__ void small_core(const SmallCore& p, const Pol& pol, unsigned char* smem, unsigned block, unsigned blocks) {

@@ -129,8 +129,8 @@ def check_product(y, q, s, wq, ws, bias, rows, expert, dtype):
         assert worst <= 1, (e, worst)
 
 
-# tokens, K, NC, experts, per token, vExperts: one row; few rows with and without segments; K in no whole stages; 256 x 256 tiles, K in whole
-# rounds of 256 and not; one expert
+# tokens, K, NC, experts, per token, vExperts: one row; few rows with and without segments; K in no whole stages; 256 x 256 tiles (2056 columns); many
+# rows on 64-row tiles, in two segments; one expert on 256 x 256 tiles
 PRODUCTS = [(1, 16, 8, 1, 1, 1), (3, 64, 72, 4, 2, 5), (16, 2048, 512, 8, 2, 12), (130, 336, 912, 12, 3, 15), (900, 272, 256, 4, 1, 9),
             (2500, 2048, 2056, 4, 3, 6), (7300, 2048, 1000, 3, 1, 3), (7300, 2064, 1024, 3, 1, 3), (7300, 2048, 2048, 1, 1, 1)]
 
