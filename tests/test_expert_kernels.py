@@ -257,3 +257,43 @@ def test_experts_that_do_not_fit():
     for wrong in (dict(sizes=(1, 16, 32)), dict(sizes=(2, 32, 32)), dict(sizes=(2, 16, 16)), dict(gated=True), dict(b1=new(2, 32)), dict(b2=new(2, 16))):
         with pytest.raises(ValueError):
             m.forward_i8(new(4, 16), new(16, 2), SimpleNamespace(**{**fits, **wrong}), [0, 1, 2], [0, 1])
+
+
+# ---- a gated layer as a whole ------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["silu", "gelu_erf"])
+@pytest.mark.parametrize("N,d,f", [(24, 64, 72), (600, 256, 512), (3000, 200, 264)])
+def test_gated_layer_is_its_formula(N, d, f, act, dtype):
+    """Output and every gradient (the gate's too) of a layer with biases and replicas against autograd in 64 bits, for the experts that the
+    layer's gate chose.  Largest error over largest value as in the other layers' parity tests: fp32 1e-5; bf16 2e-2, of which a value's four
+    or five roundings of 2^-9 on its way take a part."""
+    from paper_2304_03946_amd import layer as L
+    B = _b()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N + f)
+    E, k, V = 8, 2, 10
+
+    def new(*s, std):
+        return (torch.randn(*s, generator=gen, device="cuda") * std).to(DT[dtype])
+    t = dict(x=new(N, d, std=1), wg=new(d, E, std=d ** -0.5), w1=new(E, d, 2 * f, std=d ** -0.5), w2=new(E, f, d, std=f ** -0.5), b1=new(E, 2 * f, std=0.1),
+             b2=new(E, d, std=0.1))
+    dy = new(N, d, std=1)
+    off, ids = np.array([0, 2, 4, 5, 6, 7, 8, 9, 10], np.int32), np.arange(10, dtype=np.int32)
+    m = L.MoELayer(N, d, f, E, k, V, B.BF16 if dtype == "bf16" else B.F32, dict(silu=B.SILU, gelu_erf=B.GELU_ERF)[act], backward=True, gated=True)
+    y = m.forward(t["x"], t["wg"], t["w1"], t["w2"], off, ids, t["b1"], t["b2"]).clone()
+    got = {n: g.clone() for n, g in m.backward_full(dy, t["wg"], t["w1"], t["w2"]).items()}
+    idx = m.topk_idx.long().cpu()
+    p = {n: v.double().cpu().requires_grad_() for n, v in t.items()}
+    weight = torch.softmax(torch.gather(p["x"] @ p["wg"], 1, idx), 1)
+    want = torch.zeros(N, d, dtype=torch.float64)
+    for e in range(E):
+        tok, slot = torch.nonzero(idx == e, as_tuple=True)
+        g, up = (p["x"][tok] @ p["w1"][e] + p["b1"][e]).split(f, 1)
+        a = g * torch.sigmoid(g) if act == "silu" else g * 0.5 * torch.erfc(-g / 2 ** 0.5)
+        want = want.index_add(0, tok, weight[tok, slot][:, None] * ((a * up) @ p["w2"][e] + p["b2"][e]))
+    want.backward(dy.double().cpu())
+    pairs = {"y": (y, want.detach()), **{n: (got["d" + n], p[n].grad) for n in p}}
+    for name, (v, ref) in pairs.items():
+        err = float((v.double().cpu() - ref).abs().max() / ref.abs().max())
+        assert err <= (2e-2 if dtype == "bf16" else 1e-5), (name, err)
