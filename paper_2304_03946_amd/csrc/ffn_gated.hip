@@ -18,10 +18,13 @@
 // Rounding: H is made of the fp32 sums and rounded once.  What is kept of G and U for the backward pass are 16-bit words with two mantissa
 // bits more than bf16 has (keep4): as bf16 they put as much error into the gradients as the rounding of dHpre that cannot be
 // avoided (rel. error of dW1 and dX, 64-bit formula: 0.0030 with bf16 words, 0.0024 with these, 0.0017 is the rounding of the output alone).
+// The price: outside [2^-20, 2^12) the words have one bit less than bf16.
 //
 // What bounds them: the matrix cores where there are hundreds of rows per expert, the weights' bytes where there are few.  Measured:
-// 32768 tokens x 2, d 2048, f 5632, 32 experts: first product 2.86 ms (1.06 PFLOP/s), Y 1.25 (1.21), dH 1.75 (0.87), dX 2.68 (1.13), both weight
-// gradients 4.43 (1.02); a large library product runs at 1.42.  16 tokens x 2, d 1024, f 4096, 17 experts with rows on average: 427 MB of weights in 89 - 105 us.
+// 32768 tokens x 2, d 2048, f 5632, 32 experts: first product 2.85 ms (1.06 PFLOP/s), Y 1.31 (1.15), dH 1.72 (0.88), dX 2.70 (1.12), both weight
+// gradients 4.38 (1.03); a large library product runs at 1.42.  16 tokens x 2, d 1024, f 4096: 434 MB of weights fetched in 97 us (4.5 TB/s).
+// Registers: of the ragged 256 x 256 kernels the first product's spills 16, the others 0 to 8, reloaded in a tile's last four K tiles and its epilogue, not
+// in the steady loop; gated_small_bf16<64, FWD1, GATE_TURNS> spills 36 (fetched partial tiles, sums and accumulators together), none in the K loop.
 #include <algorithm>
 
 #include "common.h"

@@ -10,11 +10,16 @@
 // epilogue makes H = act(z) or act(g) * u in fp32, stores it in the layer's dtype and takes the largest |H| of every row (before that
 // rounding) with integer atomics on its bits -- a maximum does not depend on their order; a pass over H makes its integers, and the second
 // product reads them.  H has to be complete before its row's scale is known, so it goes through memory once as dtype and once as integers:
-// 6 bytes per element (bf16): 0.21 of 2.53 ms at 32768 tokens x 2, d 2048, f 5632.
+// 6 bytes per element (bf16): 0.21 of 2.42 ms at 32768 tokens x 2, d 2048, f 5632.  As bf16, H is rounded before its integers are, on a grid of
+// half integers from 64 on: that adds 0.2 % (SiLU gates of normal numbers, 0.5 % of them that large) or 0.8 % (GELU without a gate, 2.9 %) to the
+// error that 8 bits leave in H (6.5 % if half of a row is that large), where fp32 would add 4 bytes per element: 1.5 GB at that size.
 //
-// What bounds them: the matrix cores at hundreds of rows per expert (there, gated, both products 2.0 Pop/s; a large library product reaches
-// 2.47), the weights' bytes at few (48 tokens x 2, d 2048, f 4096, 64 experts: 1.0 GB in 213 - 226 us), launches and first loads between (one token
-// x 2, d 1024, f 4096: 4.0, 11.9, 4.0 and 7.7 us).
+// What bounds them: the matrix cores at hundreds of rows per expert (there, gated, both products 2.1 Pop/s; a large library product reaches
+// 2.47), the weights' bytes at few (48 tokens x 2, d 2048, f 4096, 64 experts: 1.06 GB fetched in 216 us), launches and first loads between (one token
+// x 2, d 1024, f 4096: 4.0, 12.0, 3.8 and 7.5 us).  A few thousand rows are bound by no unit: 3001 tokens x 2, d 784, f 2064, 16 experts keep matrix
+// pipes and LDS busy for 9 to 14 % of the cycles.
+// Registers: the 256 x 256 kernels spill 1 to 4 around a tile's K loop, the ragged forms up to 10, the bf16 one of I8_ACT 35; the steady K loops reload
+// nothing, the last four K tiles of that last kernel do (32768 tokens x 2, f 8192, GELU: d 2048 2.74 ms, d 2064, nine rounds instead of eight, 3.26).
 #include <algorithm>
 
 #include "common.h"

@@ -62,7 +62,9 @@ class MoELayer:
         """keep_h (training layers; default on): the forward pass leaves act(Hpre) in a buffer of the layer's
         and the backward pass reads it there instead of computing and storing it again -- A*f more elements
         of saved activations for a shorter backward pass.
-        gated: w1 is [E, d, 2 f], the gate's columns first; b1 [E, 2 f].  f stays the width of the hidden activations."""
+        gated: w1 is [E, d, 2 f], the gate's columns first; b1 [E, 2 f].  f stays the width of the hidden activations.  self.hpre of a gated
+        bf16 layer holds the 16-bit words that include/flexmoe.h describes, not bf16 numbers, whatever the tensor's type says.
+        A layer that only ever serves 8-bit experts holds the other passes' buffers as well."""
         self.N, self.d, self.f, self.E, self.k, self.V = N, d, f, E, k, V
         self.A = N * k
         self.act = act
