@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from test_gated_ffn import SPREAD, Case, act64, decode, dot, float32_by_default, sums  # noqa: F401
+from test_i8_experts import Ffn
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 LARGE = (1e19, -1e19, 6e19, -6e19, 1e25, -1e25, 1e33, -1e33, 30.0, -30.0)
@@ -154,3 +155,49 @@ def test_fp32_activations_of_8_bit_experts(act, gated):
     tol = 2.0 ** -21 * want.abs() + (2.0 ** -22 * z.double().abs() if act.startswith("gelu") else 0) + 1e-43
     worst = (got - want).abs() / tol
     assert float(worst.max()) <= 1, (float(z[worst.argmax()]), float(worst.max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_weight_channels_that_are_not_finite(bad, dtype):
+    """Their scale is NaN and their integers are zeros; the other channels are as without them, and what is multiplied by them is NaN."""
+    B = _b()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    E, K, NC = 2, 80, 72
+    w = torch.randn(E, K, NC, generator=gen, device="cuda").to(DT[dtype])
+
+    def quantized():
+        q, s = torch.full((E, NC, K), 99, dtype=torch.int8, device="cuda"), torch.full((E, NC), 9.0, device="cuda")
+        B.flexmoe_quantize_weights(w, q, s)
+        return q, s
+    q0, s0 = quantized()
+    w[1, 79, 65] = bad
+    q, s = quantized()
+    other = torch.ones(E, NC, dtype=torch.bool, device="cuda")
+    other[1, 65] = False
+    assert torch.isnan(s[1, 65]) and not q[1, 65].any()
+    assert torch.equal(s[other], s0[other]) and torch.equal(q[other], q0[other])
+    i32 = dict(dtype=torch.int32, device="cuda")
+    x, y = torch.ones(4, K, dtype=torch.int8, device="cuda"), torch.zeros(4, NC, dtype=DT[dtype], device="cuda")
+    ws = torch.empty(B.flexmoe_i8_workspace_bytes(4, K, NC, E, 1, 2, 0), dtype=torch.uint8, device="cuda")
+    B.flexmoe_expert_matmul_i8(x, torch.ones(4, device="cuda"), None, 1, torch.tensor([0, 2, 4], **i32), torch.tensor([0, 1], **i32), q, s, None, y, ws)
+    assert torch.isnan(y[2:, 65]).all() and int(torch.isnan(y).sum()) == 2
+
+
+# few rows on 16- and 64-row tiles; 256 x 256 tiles, with a gate and without
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu_erf", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("N,d,f,E,k,V", [(5, 64, 80, 4, 2, 5), (300, 64, 80, 4, 2, 5), (4000, 2064, 2048, 4, 2, 6)])
+def test_tokens_that_are_not_finite(N, d, f, E, k, V, gated, act, dtype):
+    """A NaN or an infinity in a token makes all of that token's rows NaN, whatever the activation, and no other row."""
+    c = Ffn(N, d, f, E, k, V, gated, act, dtype, False, seed=3)
+    y = c.run().clone()
+    c.x[N // 2, 3] = float("nan")
+    c.x[N // 3, 0] = -float("inf")
+    c.run()
+    bad = (c.t.token == N // 2) | (c.t.token == N // 3)
+    assert torch.equal(c.y[~bad], y[~bad]) and torch.isnan(c.y[bad]).all() and torch.isfinite(y).all()
